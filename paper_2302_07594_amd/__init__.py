@@ -41,17 +41,34 @@ Same names as the C ABI:
                  workspace_bytes=0)
     igemm_strerror(status), igemm_kernel_name(i), igemm_num_kernels(),
     igemm_version()
+and of include/igemm_rows.h (RouteDesc, GroupedDesc, AdaptersDesc for its
+descriptors):
+    igemm_route_query(desc), igemm_i8_grouped_query(desc, num_cu=0),
+    igemm_i8_adapters_query(desc, num_cu=0) -> workspace bytes
+    igemm_route(desc, logits, ld, bias, ids, weights, offsets, order,
+                workspace=None, workspace_bytes=0, stream=None)
+    igemm_i8_grouped(desc, offsets, order, A, lda, scale_a, B, ldb, stride_b, scale_b,
+                     out, ldo, workspace=None, workspace_bytes=0, stream=None)
+    igemm_combine(tokens, top_k, n, type, Z, ldz, weights, ids, base, ld_base, out,
+                  ldo, stream=None)
+    igemm_i8_adapters(desc, A, lda, scale_a, B, ldb, scale_b, ids, down, ld_down,
+                      stride_down, up, ld_up, stride_up, ranks, scaling, out, ldo,
+                      workspace=None, workspace_bytes=0, stream=None)
 A, B, C may be integer device addresses or torch tensors (their data_ptr()).
 Tensor conveniences: gemm_i16(A, B, C) and gemm_i8(A, B, C) take 2-D CUDA
 tensors with unit stride along rows and update C in place; gemm_srs(A, B, C,
 kc, shift, round_half_up) the same with an int16 C; conv2d(X, W, Y,
-stride, pad, dil) takes contiguous NHWC / (r, s, c, k) / NHWC tensors; a workspace the
+stride, pad, dil) takes contiguous NHWC / (r, s, c, k) / NHWC tensors; route,
+grouped_i8 and combine are a sparse layer's routing, its experts' products and
+the sum of a token's results, adapters_i8 a projection with the low-rank
+adapters of many requests; a workspace the
 call needs is taken from torch's caching allocator (so the calls can be
 captured into a torch CUDA graph) and recorded on the stream the call runs
 on; the library itself allocates nothing.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -90,6 +107,27 @@ class ConvDesc(ctypes.Structure):
     _fields_ = [(f, ctypes.c_int64) for f in
                 ("n", "h", "w", "c", "k", "r", "s", "stride_h", "stride_w", "pad_h", "pad_w",
                  "dil_h", "dil_w")]
+
+
+class RouteDesc(ctypes.Structure):
+    """igemm_route_desc."""
+    _fields_ = [("tokens", ctypes.c_int64)] + \
+        [(f, ctypes.c_int) for f in ("experts", "top_k", "groups", "top_groups", "group_best",
+                                     "score", "renormalise")] + \
+        [("scale", ctypes.c_float), ("type", ctypes.c_int)]
+
+
+class GroupedDesc(ctypes.Structure):
+    """igemm_grouped_desc."""
+    _fields_ = [(f, ctypes.c_int64) for f in ("rows", "n", "k", "groups", "a_rows", "out_rows",
+                                              "slots")] + \
+        [("scatter", ctypes.c_int), ("type", ctypes.c_int)]
+
+
+class AdaptersDesc(ctypes.Structure):
+    """igemm_adapters_desc."""
+    _fields_ = [(f, ctypes.c_int64) for f in ("m", "n", "k", "adapters", "rank")] + \
+        [("type", ctypes.c_int), ("weight_type", ctypes.c_int)]
 
 
 def conv_desc(n, h, w, c, k, r, s, stride=(1, 1), pad=(0, 0), dil=(1, 1)) -> ConvDesc:
@@ -156,6 +194,20 @@ def _load():
     lib.igemm_srs_ws.argtypes = [ci, i64, i64, i64, vp, i64, vp, i64, vp, i64, i64, ci, ci, vp,
                                  ci, vp, i64]
     lib.igemm_srs_ws.restype = ci
+    rd, gd = ctypes.POINTER(RouteDesc), ctypes.POINTER(GroupedDesc)
+    ad = ctypes.POINTER(AdaptersDesc)
+    for name, args in (
+            ("igemm_route_query", [rd, ctypes.POINTER(i64)]),
+            ("igemm_route", [rd, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp]),
+            ("igemm_i8_grouped_query", [gd, ci, ctypes.POINTER(i64)]),
+            ("igemm_i8_grouped", [gd, vp, vp, vp, i64, vp, vp, i64, i64, vp, vp, i64, vp, i64,
+                                  vp]),
+            ("igemm_combine", [i64, i64, i64, ci, vp, i64, vp, vp, vp, i64, vp, i64, vp]),
+            ("igemm_i8_adapters_query", [ad, ci, ctypes.POINTER(i64)]),
+            ("igemm_i8_adapters", [ad, vp, i64, vp, vp, i64, vp, vp, vp, i64, i64, vp, i64, i64,
+                                   vp, vp, vp, i64, vp, i64, vp])):
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = ci
     lib.igemm_conv2d_out_dim.argtypes = [i64] * 5
     lib.igemm_conv2d_out_dim.restype = i64
     lib.igemm_query_plan.argtypes = [ci, i64, i64, i64, vp, i64, vp, i64, vp, i64, ci, ci, ci,
@@ -779,3 +831,313 @@ def conv2d(X, W, Y, stride=(1, 1), pad=(0, 0), dil=(1, 1), stream=None, kernel=-
     if st != IGEMM_OK:
         raise IgemmError(st, "conv2d")
     return Y
+
+
+# ---- products whose rows choose their weights ----------------------------------
+
+IGEMM_F32, IGEMM_BF16, IGEMM_F16 = 0, 1, 2
+IGEMM_SOFTMAX, IGEMM_SIGMOID = 0, 1
+
+
+def _query(name, desc, *args) -> int:
+    out = ctypes.c_int64(0)
+    st = int(getattr(_lib, name)(None if desc is None else ctypes.byref(desc), *args,
+                                 ctypes.byref(out)))
+    if st != IGEMM_OK:
+        raise IgemmError(st, name)
+    return int(out.value)
+
+
+def igemm_route_query(desc) -> int:
+    """Workspace bytes igemm_route needs. Host only; raises IgemmError for an
+    invalid descriptor, as the two queries below."""
+    return _query("igemm_route_query", desc)
+
+
+def igemm_i8_grouped_query(desc, num_cu=0) -> int:
+    return _query("igemm_i8_grouped_query", desc, int(num_cu))
+
+
+def igemm_i8_adapters_query(desc, num_cu=0) -> int:
+    return _query("igemm_i8_adapters_query", desc, int(num_cu))
+
+
+def igemm_route(desc, logits, ld, bias, ids, weights, offsets, order, workspace=None,
+                workspace_bytes=0, stream=None) -> int:
+    """Routing (see include/igemm_rows.h). Returns the status."""
+    return int(_lib.igemm_route(ctypes.byref(desc), _addr(logits), int(ld), _addr(bias),
+                                _addr(ids), _addr(weights), _addr(offsets), _addr(order),
+                                _addr(workspace), int(workspace_bytes), _stream(stream)))
+
+
+def igemm_i8_grouped(desc, offsets, order, A, lda, scale_a, B, ldb, stride_b, scale_b, out, ldo,
+                     workspace=None, workspace_bytes=0, stream=None) -> int:
+    """The experts' products (see include/igemm_rows.h). Returns the status."""
+    return int(_lib.igemm_i8_grouped(ctypes.byref(desc), _addr(offsets), _addr(order), _addr(A),
+                                     int(lda), _addr(scale_a), _addr(B), int(ldb), int(stride_b),
+                                     _addr(scale_b), _addr(out), int(ldo), _addr(workspace),
+                                     int(workspace_bytes), _stream(stream)))
+
+
+def igemm_combine(tokens, top_k, n, type, Z, ldz, weights, ids, base, ld_base, out, ldo,
+                  stream=None) -> int:
+    """The weighted sum of each token's slots. Returns the status."""
+    return int(_lib.igemm_combine(int(tokens), int(top_k), int(n), int(type), _addr(Z), int(ldz),
+                                  _addr(weights), _addr(ids), _addr(base), int(ld_base),
+                                  _addr(out), int(ldo), _stream(stream)))
+
+
+def igemm_i8_adapters(desc, A, lda, scale_a, B, ldb, scale_b, ids, down, ld_down, stride_down,
+                      up, ld_up, stride_up, ranks, scaling, out, ldo, workspace=None,
+                      workspace_bytes=0, stream=None) -> int:
+    """A projection with adapters (see include/igemm_rows.h). Returns the status."""
+    return int(_lib.igemm_i8_adapters(ctypes.byref(desc), _addr(A), int(lda), _addr(scale_a),
+                                      _addr(B), int(ldb), _addr(scale_b), _addr(ids),
+                                      _addr(down), int(ld_down), int(stride_down), _addr(up),
+                                      int(ld_up), int(stride_up), _addr(ranks), _addr(scaling),
+                                      _addr(out), int(ldo), _addr(workspace),
+                                      int(workspace_bytes), _stream(stream)))
+
+
+def _type_of(dtype, name, what):
+    import torch
+    types = {torch.float32: IGEMM_F32, torch.bfloat16: IGEMM_BF16, torch.float16: IGEMM_F16}
+    if dtype not in types:
+        raise TypeError(f"{name}: {what} must be torch.float32, bfloat16 or float16")
+    return types[dtype]
+
+
+@contextlib.contextmanager
+def _on(device, stream):
+    """The device of the tensors made current, and the stream the call runs on:
+    the device's current one, or `stream` (a torch stream or a raw handle), made
+    current too, so that what the call allocates and fills belongs to it."""
+    import torch
+    with torch.cuda.device(device):
+        if stream is None:
+            yield int(torch.cuda.current_stream().cuda_stream)
+            return
+        if not hasattr(stream, "cuda_stream") and not isinstance(stream, int):
+            raise TypeError("stream must be None, an int handle or a torch stream")
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=device)
+        with torch.cuda.stream(stream):
+            yield int(stream.cuda_stream)
+
+
+def _expect(name, what, t, dtypes, shape, device, rows=True):
+    """Type, shape (None: any) and device of a tensor whose rows have unit stride;
+    rows=False: it is dense. Returns the leading dimension of its last two."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
+        raise TypeError(f"{name}: {what} must be a tensor of {' or '.join(map(str, dtypes))}")
+    if t.dim() != len(shape) or any(w is not None and s != w for s, w in zip(t.shape, shape)):
+        want = ", ".join("any" if w is None else str(w) for w in shape)
+        raise ValueError(f"{name}: {what} must have shape ({want}), got {tuple(t.shape)}")
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name}: {what} must be a CUDA (HIP) tensor on the operands' device")
+    if t.numel() == 0:
+        return max(t.shape[-1], 1)
+    if not rows:
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: {what} must be contiguous")
+        return max(t.shape[-1], 1)
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: {what} must have unit stride along rows")
+    ld = t.stride(-2) if t.dim() > 1 and t.shape[-2] > 1 else max(t.shape[-1], 1)
+    return ld
+
+
+def _space(name, workspace, nbytes, device):
+    """(workspace, bytes): the caller's, or one from torch's caching allocator."""
+    if workspace is None:
+        return (_aligned_workspace(nbytes, device), nbytes) if nbytes > 0 else (None, 0)
+    if not hasattr(workspace, "data_ptr"):
+        raise ValueError(f"{name}: workspace must be None or a tensor")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def route(logits, top_k, bias=None, groups=1, top_groups=1, group_best=1, score="softmax",
+          renormalise=True, scale=1.0, plan=True, stream=None, workspace=None):
+    """Choose top_k experts for every row of logits (tokens x experts, a CUDA tensor
+    of float32, bfloat16 or float16 with unit stride along rows).
+
+    score: "softmax" or "sigmoid"; bias: float32, one an expert, added to the scores
+    for the choice only; groups, top_groups, group_best: the experts form `groups`
+    runs, of which the top_groups with the largest sum of their group_best (1 or
+    2) best stay; renormalise: the weights of a token add up to scale. Experts
+    whose logit is -inf or NaN are not chosen; ties go to the lower index.
+
+    Returns (ids, weights, offsets, order): int32 and float32 (tokens, top_k), with
+    id -1 and weight 0 where no expert is left, and the plan that grouped_i8
+    takes, int32 (experts + 1) and (tokens * top_k); plan=False leaves the plan
+    out (None, None). workspace as for gemm_i16 (None or a uint8 tensor)."""
+    import torch
+    f = (torch.float32, torch.bfloat16, torch.float16)
+    ld = _expect("route", "logits", logits, f, (None, None), None)
+    tokens, experts = logits.shape
+    if bias is not None:
+        _expect("route", "bias", bias, (torch.float32,), (experts,), logits.device, rows=False)
+    if score not in ("softmax", "sigmoid"):
+        raise ValueError("route: score must be 'softmax' or 'sigmoid'")
+    desc = RouteDesc(tokens, experts, int(top_k), int(groups), int(top_groups), int(group_best),
+                     IGEMM_SIGMOID if score == "sigmoid" else IGEMM_SOFTMAX,
+                     1 if renormalise else 0, float(scale),
+                     _type_of(logits.dtype, "route", "logits"))
+    nbytes = igemm_route_query(desc)
+    with _on(logits.device, stream) as s:
+        new = dict(device=logits.device, dtype=torch.int32)
+        ids = torch.empty((tokens, int(top_k)), **new)
+        weights = torch.empty((tokens, int(top_k)), device=logits.device)
+        offsets = torch.empty(experts + 1, **new) if plan else None
+        order = torch.empty(tokens * int(top_k), **new) if plan else None
+        ws, ws_bytes = _space("route", workspace, nbytes, logits.device)
+        st = igemm_route(desc, logits, ld, bias, ids, weights, offsets, order, ws, ws_bytes, s)
+    if st != IGEMM_OK:
+        raise IgemmError(st, "route")
+    return ids, weights, offsets, order
+
+
+def grouped_i8(A, B, offsets, order=None, scale_a=None, scale_b=None, slots=0, scatter=False,
+               rows=None, out=None, out_dtype=None, stream=None, workspace=None):
+    """The experts' products: position i of group g (offsets[g] <= i < offsets[g + 1])
+    multiplies a row of A with B[g].
+
+    A: a_rows x k int8, B: groups x k x n int8 (each group's matrix with unit stride
+    along rows), offsets: int32 (groups + 1), order: int32 (rows) or None (the
+    positions themselves); scale_a float32 (a_rows), scale_b float32 (groups, n),
+    or None. The row of A is the position, or order[i] // slots for slots > 0 (slots
+    = top_k: the token); the row of out is the position, or order[i] with scatter.
+    rows: the number of positions, if order is None (default: A's rows).
+
+    out: (out_rows, n) float32, bfloat16 or float16 with unit stride along rows,
+    overwritten where a position leads; None: a zeroed (rows, n) tensor of out_dtype
+    (default bfloat16). Returns out. Raises IgemmError on a bad status."""
+    import torch
+    i8, i32, f32 = (torch.int8,), (torch.int32,), (torch.float32,)
+    lda = _expect("grouped_i8", "A", A, i8, (None, None), None)
+    a_rows, k = A.shape
+    ldb = _expect("grouped_i8", "B", B, i8, (None, k, None), A.device)
+    groups, _, n = B.shape
+    stride_b = B.stride(0) if groups > 1 and B.numel() > 0 else 0
+    _expect("grouped_i8", "offsets", offsets, i32, (groups + 1,), A.device, rows=False)
+    if order is not None:
+        _expect("grouped_i8", "order", order, i32, (rows,), A.device, rows=False)
+        rows = order.shape[0]
+    elif rows is None:
+        rows = a_rows
+    if scale_a is not None:
+        _expect("grouped_i8", "scale_a", scale_a, f32, (a_rows,), A.device, rows=False)
+    if scale_b is not None:
+        _expect("grouped_i8", "scale_b", scale_b, f32, (groups, n), A.device, rows=False)
+    f = (torch.float32, torch.bfloat16, torch.float16)
+    if out is not None:
+        _expect("grouped_i8", "out", out, f if out_dtype is None else (out_dtype,), (None, n),
+                A.device)
+    dtype = out.dtype if out is not None else (out_dtype or torch.bfloat16)
+    with _on(A.device, stream) as s:
+        if out is None:
+            _type_of(dtype, "grouped_i8", "out_dtype")
+            out = torch.zeros((rows, n), dtype=dtype, device=A.device)
+        ldo = out.stride(0) if out.shape[0] > 1 and out.numel() > 0 else max(n, 1)
+        desc = GroupedDesc(rows, n, k, groups, a_rows, out.shape[0], int(slots),
+                           1 if scatter else 0, _type_of(dtype, "grouped_i8", "out"))
+        nbytes = igemm_i8_grouped_query(desc, _num_cu(A.device))
+        ws, ws_bytes = _space("grouped_i8", workspace, nbytes, A.device)
+        st = igemm_i8_grouped(desc, offsets, order, A, lda, scale_a, B, ldb, stride_b, scale_b,
+                              out, ldo, ws, ws_bytes, s)
+    if st != IGEMM_OK:
+        raise IgemmError(st, "grouped_i8")
+    return out
+
+
+def combine(Z, weights, ids=None, base=None, out=None, stream=None):
+    """out[t] = base[t] + the sum over j of weights[t, j] * Z[t * top_k + j], slots with
+    ids[t, j] < 0 left out. Z: (tokens * top_k, n) float32, bfloat16 or float16, unit
+    stride along rows; weights: float32 (tokens, top_k), contiguous; ids: int32 of
+    that shape or None; base and out: (tokens, n) of Z's type (out may be base; None:
+    a new tensor). Returns out."""
+    import torch
+    f = (torch.float32, torch.bfloat16, torch.float16)
+    _expect("combine", "weights", weights, (torch.float32,), (None, None), None, rows=False)
+    tokens, top_k = weights.shape
+    dev = weights.device
+    ldz = _expect("combine", "Z", Z, f, (tokens * top_k, None), dev)
+    n = Z.shape[1]
+    if ids is not None:
+        _expect("combine", "ids", ids, (torch.int32,), (tokens, top_k), dev, rows=False)
+    ld_base = 0
+    if base is not None:
+        ld_base = _expect("combine", "base", base, (Z.dtype,), (tokens, n), dev)
+    if out is not None:
+        _expect("combine", "out", out, (Z.dtype,), (tokens, n), dev)
+    with _on(dev, stream) as s:
+        if out is None:
+            out = torch.empty((tokens, n), dtype=Z.dtype, device=dev)
+        ldo = out.stride(0) if tokens > 1 and n > 0 else max(n, 1)
+        st = igemm_combine(tokens, top_k, n, _type_of(Z.dtype, "combine", "Z"), Z, ldz, weights,
+                           ids, base, ld_base, out, ldo, s)
+    if st != IGEMM_OK:
+        raise IgemmError(st, "combine")
+    return out
+
+
+def adapters_i8(A, B, ids=None, down=None, up=None, scale_a=None, scale_b=None, ranks=None,
+                scaling=None, out=None, out_dtype=None, stream=None, workspace=None):
+    """The projection scale_a * scale_b * (A.B) of int8 A (m x k) and B (k x n) and, beside
+    it, for row i with adapter a = ids[i] (-1: none),
+    scaling[a] * (scale_a[i] * A[i] . down[a]^T) . up[a]^T.
+
+    down: (adapters, rank, k) and up: (adapters, n, rank), both bfloat16 or both
+    float16, unit stride along rows; ids: int32 (m); ranks: int32 (adapters) or
+    None; scale_a float32 (m), scale_b float32 (n), scaling float32 (adapters), or
+    None. ids, down and up are given together; without them: the projection alone.
+    out: (m, n) float32, bfloat16 or float16 with unit stride along rows; None: a new
+    tensor of out_dtype (default bfloat16). Returns out."""
+    import torch
+    i8, i32, f32 = (torch.int8,), (torch.int32,), (torch.float32,)
+    name = "adapters_i8"
+    lda = _expect(name, "A", A, i8, (None, None), None)
+    m, k = A.shape
+    dev = A.device
+    ldb = _expect(name, "B", B, i8, (k, None), dev)
+    n = B.shape[1]
+    if scale_a is not None:
+        _expect(name, "scale_a", scale_a, f32, (m,), dev, rows=False)
+    if scale_b is not None:
+        _expect(name, "scale_b", scale_b, f32, (n,), dev, rows=False)
+    given = [x is not None for x in (ids, down, up)]
+    if any(given) != all(given):
+        raise ValueError(f"{name}: ids, down and up are given together")
+    adapters = rank = ld_down = ld_up = stride_down = stride_up = 0
+    wt = IGEMM_BF16
+    if all(given):
+        h = (torch.bfloat16, torch.float16)
+        ld_down = _expect(name, "down", down, h, (None, None, k), dev)
+        adapters, rank, _ = down.shape
+        ld_up = _expect(name, "up", up, (down.dtype,), (adapters, n, rank), dev)
+        _expect(name, "ids", ids, i32, (m,), dev, rows=False)
+        stride_down = down.stride(0) if adapters > 1 and down.numel() > 0 else 0
+        stride_up = up.stride(0) if adapters > 1 and up.numel() > 0 else 0
+        wt = _type_of(down.dtype, name, "down")
+        if ranks is not None:
+            _expect(name, "ranks", ranks, i32, (adapters,), dev, rows=False)
+        if scaling is not None:
+            _expect(name, "scaling", scaling, f32, (adapters,), dev, rows=False)
+    f = (torch.float32, torch.bfloat16, torch.float16)
+    if out is not None:
+        _expect(name, "out", out, f if out_dtype is None else (out_dtype,), (m, n), dev)
+    dtype = out.dtype if out is not None else (out_dtype or torch.bfloat16)
+    desc = AdaptersDesc(m, n, k, adapters, rank, _type_of(dtype, name, "out_dtype"), wt)
+    nbytes = igemm_i8_adapters_query(desc, _num_cu(dev))
+    with _on(dev, stream) as s:
+        if out is None:
+            out = torch.empty((m, n), dtype=dtype, device=dev)
+        ldo = out.stride(0) if m > 1 and n > 0 else max(n, 1)
+        ws, ws_bytes = _space(name, workspace, nbytes, dev)
+        st = igemm_i8_adapters(desc, A, lda, scale_a, B, ldb, scale_b, ids, down, ld_down,
+                               stride_down, up, ld_up, stride_up, ranks, scaling, out, ldo, ws,
+                               ws_bytes, s)
+    if st != IGEMM_OK:
+        raise IgemmError(st, name)
+    return out
