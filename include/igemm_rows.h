@@ -102,8 +102,8 @@ int igemm_route(const igemm_route_desc *desc, const void *logits, int64_t ld, co
  * left as they were; if two positions name one row of out, one of them is kept.
  * A position whose row of A or out is outside a_rows or out_rows is skipped.
  *
- *   offsets  groups + 1 int32, ascending; values outside [0, rows] act as the
- *            nearest bound.
+ *   offsets  groups + 1 int32, ascending (or the values of out are not specified);
+ *            values outside [0, rows] act as the nearest bound.
  *   order    rows int32, or NULL.
  *   A        a_rows x k int8, row-major, leading dimension lda >= k.
  *   scale_a  a_rows floats or NULL.
@@ -117,8 +117,8 @@ int igemm_route(const igemm_route_desc *desc, const void *logits, int64_t ld, co
  *
  * Errors: IGEMM_EINVAL as for igemm_i8, and for slots < 0, scatter not 0 or 1 or
  * an unknown type; IGEMM_ENOTSUP for k beyond 131071 (sums past 2^31), extents
- * beyond 2^31 - 1, more than 65536 groups, or an A, a matrix of B, or 256 rows
- * of out of 2 GiB or more. rows = 0 or n = 0: IGEMM_OK, out unchanged. k = 0: zeros.
+ * beyond 2^31 - 1, more than 65536 groups, an A or a matrix of B within 256 bytes of
+ * 2 GiB or over, or 256 rows of out of 2 GiB or more. rows = 0 or n = 0: IGEMM_OK, out unchanged. k = 0: zeros.
  */
 typedef struct igemm_grouped_desc {
     int64_t rows, n, k, groups;

@@ -70,7 +70,8 @@ int check_operands(int64_t a_rows, int64_t n, int64_t k, const void *A, int64_t 
     if (A == nullptr || B == nullptr || lda < k || ldb < n) return IGEMM_EINVAL;
     if (lda > kMax || ldb > kMax) return IGEMM_ENOTSUP;
     const int64_t a = extent(a_rows, k, lda, 1), b = extent(k, n, ldb, 1);
-    if (a < 0 || a > kMax || b < 0 || b > kMax) return IGEMM_ENOTSUP;
+    // (32-bit offsets, of a k-tile that may reach past the end)
+    if (a < 0 || a > kMax - 256 || b < 0 || b > kMax - 256) return IGEMM_ENOTSUP;
     return IGEMM_OK;
 }
 

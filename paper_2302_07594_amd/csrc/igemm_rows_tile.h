@@ -1,0 +1,468 @@
+// Tile kernel of the experts' products and of the shared projection with
+// adapters: out rows = scales * (A rows . B of the row's group) (+ adapters).
+//
+// The inner product is the ring kernel's (igemm_ring.h): A and B move into
+// LDS as they lie, by buffer DMA where rows start at 4-byte addresses, else
+// through registers; B is turned k-contiguous by the transpose reads. What
+// differs:
+//   * the grid covers the most row tiles that the sizes allow, and a workgroup
+//     finds its group and rows from the offsets on the device (one wave scan);
+//     workgroups past the last tile leave at once, so nothing is read back by
+//     the host;
+//   * a lane's DMA address takes its row of A from the plan, so gathering rows
+//     costs nothing more than reading consecutive ones;
+//   * the sums are int32 and exact (k <= 131071); they are scaled in float,
+//     turned to rows of 16-byte pieces through LDS and stored once, where the
+//     raw sums would cost two more passes over four bytes an element.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "igemm_ring.h"
+#include "igemm_rows_device.h"
+
+namespace igemm {
+namespace rows {
+
+using lds::tr8;
+using lds::v2i;
+using ring::v4u;
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+
+// The ring of k-tiles: 128 k, one whole line of a row of A.
+constexpr int kStepK = 128;
+
+// 8 values as bf16 parts hi + mid + lo, each the rounding of what the ones
+// before it leave: 24 bits together. An infinite or NaN value is its hi alone.
+__device__ __forceinline__ void split3(const float *x, v8bf &hi, v8bf &mid, v8bf &lo) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const __bf16 h = (__bf16)x[e];
+        const float r = x[e] - (float)h;
+        const bool fine = r == r;
+        const __bf16 m = fine ? (__bf16)r : (__bf16)0.0f;
+        hi[e] = h;
+        mid[e] = m;
+        lo[e] = fine ? (__bf16)(r - (float)m) : (__bf16)0.0f;
+    }
+}
+
+// 8 consecutive 16-bit values of a row of `len`, from element e0; zero from
+// `used` on.
+__device__ __forceinline__ void load8(const uint16_t *row, int e0, int len, int used, u32 w[4]) {
+    if (e0 + 8 <= len) {
+        const v4i v = ring::load_u16((const char *)(row + e0));
+        w[0] = (u32)v.x;
+        w[1] = (u32)v.y;
+        w[2] = (u32)v.z;
+        w[3] = (u32)v.w;
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            w[q] = e0 + 2 * q < len ? row[e0 + 2 * q] : 0u;
+            if (e0 + 2 * q + 1 < len) w[q] |= (u32)row[e0 + 2 * q + 1] << 16;
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int left = used - e0 - 2 * q;
+        w[q] = left >= 2 ? w[q] : (left == 1 ? w[q] & 0xffffu : 0u);
+    }
+}
+
+__device__ __forceinline__ int rank_of(const Adapters &ad, int which) {
+    if (which < 0 || which >= ad.adapters) return 0;
+    return ad.ranks != nullptr ? min(max(ad.ranks[which], 0), ad.rank) : ad.rank;
+}
+
+// BM x BN: the workgroup's tile, WM x WN a wave's; NST ring stages; OCC
+// workgroups a compute unit; REG: through registers; PART: the raw sums of k
+// slice z go to part[z][position][column] instead; ADAPT: adapters beside, with
+// u in ks parts of rows x rpad floats.
+template <int BM, int BN, int WM, int WN, int NST, int OCC, bool REG, bool PART, bool ADAPT>
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, OCC *((BM / WM) * (BN / WN)) / 4)
+rows_tile(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
+          int32_t *__restrict__ part, int slices, int kchunk) {
+    typedef Mfma<32> M;
+    constexpr int TM = WM / 32, TN = WN / 32;
+    constexpr int WGN = BN / WN, NW = (BM / WM) * WGN;
+    constexpr int BK = kStepK, RA = BK, RB = BN;
+    constexpr int APL = BM * RA, BPL = BK * RB, STAGE = APL + BPL;
+    constexpr int RPA = 1024 / RA, RPB = 1024 / RB;
+    static_assert(APL % (1024 * NW) == 0 && BPL % (1024 * NW) == 0, "1 KB blocks per wave");
+    constexpr int DPA = APL / 1024 / NW, DPB = BPL / 1024 / NW, DPW = DPA + DPB;
+    static_assert(NST >= 2 && (NST - 2) * DPW < 64, "outstanding DMA count");
+    static_assert(!REG || NST == 2, "two stages through registers");
+    static_assert(OCC * (NST * STAGE + 16 * BM) <= 160 * 1024, "LDS");
+    // A wave's output block of 32 rows, in pieces of 16 bytes.
+    constexpr int PITCH = WN * 4 + 16;
+    static_assert(NW * 32 * PITCH <= NST * STAGE, "output blocks fit the ring");
+
+    __shared__ __attribute__((aligned(1024))) char smem[NST * STAGE];
+    __shared__ __attribute__((aligned(16))) int arow[BM], orow[BM], arow_id[BM];
+    __shared__ __attribute__((aligned(16))) float arow_s[BM];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm0 = (wave / WGN) * WM, wn0 = (wave % WGN) * WN;
+
+    // ---- which tile -----------------------------------------------------------
+    const int tiles_n = (p.n + BN - 1) / BN;
+    const int per = (p.groups + 63) / 64;
+    int before;
+    const int row_tiles = wave_tiles(p, BM, per, lane, &before);
+    // Workgroup ids go to the eight XCDs in turn: each takes a contiguous range
+    // of the tiles, so that tiles that run together share A and B in its L2.
+    const int64_t total = (int64_t)row_tiles * tiles_n * slices;
+    int64_t at;
+    {
+        const int64_t q = total >> 3;
+        const int r = (int)(total & 7), x = blockIdx.x & 7, i = blockIdx.x >> 3;
+        if (i >= q + (x < r)) return;
+        at = x * q + min(x, r) + i;
+    }
+    const int z = (int)(at % slices), t = (int)(at / slices);
+    const Found f = wave_find(p, BM, per, lane, before, t / tiles_n);
+    // Within a group: eight row tiles at a time, over all columns.
+    int m0, n0;
+    {
+        const int mt = (f.cnt + BM - 1) / BM;
+        const int in = t - f.pre * tiles_n, span = 8 * tiles_n;
+        const int first = in / span * 8, gsize = min(mt - first, 8);
+        const int rest = in - in / span * span;
+        m0 = (first + rest % gsize) * BM;
+        n0 = rest / gsize * BN;
+    }
+    const int mrows = min(f.cnt - m0, BM);
+    const int kbeg = z * kchunk, klen = min(p.k - kbeg, kchunk);
+    const int nkt = (klen + BK - 1) / BK;
+
+    for (int r = tid; r < BM; r += NW * 64) {
+        int a = -1, o = -1;
+        if (r < mrows) rows_of(p, f.lo + m0 + r, &a, &o);
+        arow[r] = a;
+        orow[r] = o;
+        if constexpr (!PART) arow_s[r] = a >= 0 && p.scale_a != nullptr ? p.scale_a[a] : 1.0f;
+        if constexpr (ADAPT) {
+            const int w = a >= 0 ? ad.ids[a] : -1;
+            arow_id[r] = w >= 0 && w < ad.adapters ? w : -1;
+        }
+    }
+    __syncthreads();
+
+    // ---- staging ----------------------------------------------------------------
+    int a_row[DPA], a_lc[DPA], b_row[DPB], b_lc[DPB];
+#pragma unroll
+    for (int d = 0; d < DPA; ++d) {
+        a_row[d] = (wave * DPA + d) * RPA + lane / (RA / 16);
+        a_lc[d] = (lane % (RA / 16)) ^ (REG ? 0 : ring::swz_a<RA>(a_row[d]));
+    }
+#pragma unroll
+    for (int d = 0; d < DPB; ++d) {
+        b_row[d] = (wave * DPB + d) * RPB + lane / (RB / 16);
+        b_lc[d] = (lane % (RB / 16)) ^ (REG ? 0 : ring::swz_b<RB>(b_row[d]));
+    }
+    const int lda = (int)p.lda, ldb = (int)p.ldb;
+    const char *a_base = (const char *)p.A + kbeg;
+    const char *b_base = (const char *)p.B + f.group * p.stride_b + (int64_t)kbeg * ldb + n0;
+    const u32 lds0 = (u32)(uintptr_t)(const __attribute__((address_space(3))) char *)smem;
+
+    u32 a_vo[DPA], b_vo[DPB];
+    v4u Ars = {0u, 0u, 0u, 0u}, Brs = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int d = 0; d < DPA; ++d) {
+        const int a = arow[a_row[d]];
+        a_vo[d] = a >= 0 ? (u32)a * (u32)lda + 16u * (u32)a_lc[d] : 0x80000000u;
+    }
+#pragma unroll
+    for (int d = 0; d < DPB; ++d) b_vo[d] = (u32)b_row[d] * (u32)ldb + 16u * (u32)b_lc[d];
+    if constexpr (!REG) {
+        // B's resource ends with its k range: rows beyond are zeros, so what A
+        // has beyond the range, or in rows with nothing to do, never counts.
+        Ars = ring::resource(a_base, (u32)(((int64_t)(p.a_rows - 1) * lda + p.k - kbeg + 3) & ~3));
+        Brs = ring::resource(b_base, (u32)(((int64_t)(klen - 1) * ldb + p.n - n0 + 3) & ~3));
+    }
+    auto issue = [&](int kt, int s) __attribute__((always_inline)) {
+        const bool in = kt < nkt;
+        v4u ar = Ars, br = Brs;
+        ar.z = in ? ar.z : 0u;
+        br.z = in ? br.z : 0u;
+        const u32 as = in ? (u32)(kt * BK) : 0u;
+        const u32 bs = in ? (u32)(kt * BK) * (u32)ldb : 0u;
+        const u32 base = lds0 + (u32)(s * STAGE);
+#pragma unroll
+        for (int d = 0; d < DPB; ++d)
+            ring::dma(b_vo[d] + bs, br, base + (u32)(APL + (wave * DPB + d) * 1024));
+#pragma unroll
+        for (int d = 0; d < DPA; ++d)
+            ring::dma(a_vo[d] + as, ar, base + (u32)((wave * DPA + d) * 1024));
+    };
+
+    // Through registers: bounded loads of any alignment.
+    typedef v4i regs_a[REG ? DPA : 1];
+    typedef v4i regs_b[REG ? DPB : 1];
+    auto load = [&](regs_a &va, regs_b &vb, int kt) __attribute__((always_inline)) {
+        if constexpr (REG) {
+            const int k0 = kt * BK, left = klen - k0;
+            const int a_end = (int)((int64_t)(p.a_rows - 1) * lda + p.k - kbeg);
+            const bool a_tiny = (int64_t)(p.a_rows - 1) * lda + p.k < 16;
+            const bool b_tiny = (int64_t)(p.k - 1) * ldb + p.n < 16;
+            const char *bk = b_base + (int64_t)k0 * ldb;
+            const int b_end =
+                (int)min((int64_t)(p.k - 1 - kbeg - k0) * ldb + p.n - n0, (int64_t)0x7fffffff);
+#pragma unroll
+            for (int d = 0; d < DPA; ++d) {
+                const int a = max(arow[a_row[d]], 0);
+                va[d] = ring::load_edge(a_base, a * lda + k0 + 16 * a_lc[d], a_end, a_tiny);
+            }
+#pragma unroll
+            for (int d = 0; d < DPB; ++d) {
+                const int off = min(b_row[d], left - 1) * ldb + 16 * b_lc[d];
+                vb[d] = ring::load_edge(bk, off, b_end, b_tiny);
+                if (b_row[d] >= left) vb[d] = v4i{0, 0, 0, 0};
+            }
+        }
+    };
+    auto store = [&](const regs_a &va, const regs_b &vb, int s) __attribute__((always_inline)) {
+        if constexpr (REG) {
+            char *sa = smem + s * STAGE, *sb = sa + APL;
+#pragma unroll
+            for (int d = 0; d < DPA; ++d)
+                *(v4i *)(sa + a_row[d] * RA + 16 * (a_lc[d] ^ ring::swz_a<RA>(a_row[d]))) = va[d];
+#pragma unroll
+            for (int d = 0; d < DPB; ++d)
+                *(v4i *)(sb + b_row[d] * RB + 16 * (b_lc[d] ^ ring::swz_b<RB>(b_row[d]))) = vb[d];
+        }
+    };
+
+    // ---- fragments and matrix instructions (as the ring kernel's) -----------------
+    constexpr int KS = BK / 32;
+    const int fr = lane & 31, gq = lane >> 4, ul = lane & 15;
+    int a_rd[KS], b_rd[TN];
+    {
+        const int row = wm0 + fr, krow = 16 * (gq >> 1) + (ul >> 1);
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+            a_rd[s] = row * RA + 16 * ((2 * s + (lane >> 5)) ^ ring::swz_a<RA>(row));
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int cb = wn0 + 32 * j + 16 * (gq & 1) + 8 * (ul & 1);
+            b_rd[j] = APL + krow * RB + 16 * ((cb >> 4) ^ ring::swz_b<RB>(krow)) + (cb & 15);
+        }
+    }
+    v16i acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+    auto tile = [&](int s) __attribute__((always_inline)) {
+        const char *st = smem + s * STAGE;
+#pragma unroll
+        for (int q = 0; q < KS; ++q) {
+            v4i a[TM], b[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const char *at_b = st + b_rd[j] + q * 32 * RB;
+                const v2i x = tr8(at_b), y = tr8(at_b + 8 * RB);
+                b[j] = v4i{x.x, x.y, y.x, y.y};
+            }
+#pragma unroll
+            for (int i = 0; i < TM; ++i) a[i] = *(const v4i *)(st + a_rd[q] + i * 32 * RA);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = M::mma(a[i], b[j], acc[i][j]);
+        }
+    };
+    if constexpr (!REG) {
+#pragma unroll
+        for (int s = 0; s < NST - 1; ++s) issue(s, s);
+        int s = 0;
+        for (int kt = 0; kt < nkt; ++kt) {
+            // tile kt has landed when at most the NST - 2 later ones are out
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NST - 2) * DPW)
+                         : "memory");
+            issue(kt + NST - 1, s == 0 ? NST - 1 : s - 1);
+            tile(s);
+            s = s == NST - 1 ? 0 : s + 1;
+        }
+        // no DMA may land in LDS that is used anew below
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    } else {
+        regs_a va;
+        regs_b vb;
+        if (nkt > 0) {
+            load(va, vb, 0);
+            store(va, vb, 0);
+        }
+        for (int kt = 0; kt < nkt; ++kt) {
+            __syncthreads();
+            if (kt + 1 < nkt) load(va, vb, kt + 1);
+            tile(kt & 1);
+            if (kt + 1 < nkt) store(va, vb, 1 - (kt & 1));
+        }
+    }
+
+    // ---- raw sums of a slice ----------------------------------------------------------
+    if constexpr (PART) {
+        int32_t *dst = part + ((int64_t)z * p.rows + f.lo + m0) * p.n + n0;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int c = wn0 + 32 * j + M::out_col(lane);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int lr = wm0 + 32 * i + M::out_row(lane, r);
+                    if (lr < mrows && n0 + c < p.n) dst[(int64_t)lr * p.n + c] = acc[i][j][r];
+                }
+            }
+        return;
+    }
+
+    // ---- scales, adapters, output -------------------------------------------------------
+    __syncthreads();  // the ring becomes the waves' output blocks
+    char *blk = smem + wave * 32 * PITCH;
+    float sb[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int c = n0 + wn0 + 32 * j + M::out_col(lane);
+        sb[j] = p.scale_b != nullptr && c < p.n ? p.scale_b[(int64_t)f.group * p.n + c] : 1.0f;
+    }
+    auto emit = [&](auto type_c) __attribute__((always_inline)) {
+        constexpr int T = decltype(type_c)::value;
+        constexpr int ES = T == IGEMM_F32 ? 4 : 2, V = 16 / ES, LPR = WN / V;  // lanes a row
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int r0 = wm0 + 32 * i;
+            float x[TN][16];
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const float4 s = *(const float4 *)(arow_s + r0 + M::out_row(lane, r));
+                const float sa[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+                        x[j][r + q] = (float)acc[i][j][r + q] * sa[q] * sb[j];
+            }
+            if constexpr (ADAPT) {
+                // The block's adapters, one after the other: every row is
+                // multiplied with each, and takes its own one's result. (A row
+                // of a matrix product depends on its own row of the left operand
+                // alone, so other rows' values cannot reach it.)
+                const int mine = arow_id[r0 + fr];
+                const int arow_u = max(arow[r0 + fr], 0);
+                uint64_t todo = __ballot(mine >= 0);
+                while (todo != 0) {
+                    const int which =
+                        __builtin_amdgcn_readlane(mine, __ffsll((unsigned long long)todo) - 1);
+                    todo &= ~__ballot(mine == which);
+                    const int rank = rank_of(ad, which);
+                    v16f y[TN];
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) y[j][r] = 0.0f;
+                    for (int e0 = 0; e0 < rank; e0 += 16) {
+                        const int e = e0 + 8 * (lane >> 5);
+                        float uv[8] = {};
+                        for (int q = 0; q < ks; ++q) {
+                            const float4 *src =
+                                (const float4 *)(u + ((int64_t)q * p.rows + arow_u) * rpad + e);
+                            const float4 lo = src[0], hi = src[1];
+                            uv[0] += lo.x;
+                            uv[1] += lo.y;
+                            uv[2] += lo.z;
+                            uv[3] += lo.w;
+                            uv[4] += hi.x;
+                            uv[5] += hi.y;
+                            uv[6] += hi.z;
+                            uv[7] += hi.w;
+                        }
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) uv[q] = e + q < rank ? uv[q] : 0.0f;
+                        v8bf u1, u2, u3;
+                        split3(uv, u1, u2, u3);
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) {
+                            const int c = min(n0 + wn0 + 32 * j + fr, p.n - 1);
+                            u32 w[4];
+                            load8((const uint16_t *)ad.up + which * ad.stride_up + c * ad.ld_up,
+                                  e, ad.rank, rank, w);
+                            if (ad.type == IGEMM_BF16) {
+                                const v4u b4 = {w[0], w[1], w[2], w[3]};
+                                const v8bf v = __builtin_bit_cast(v8bf, b4);
+                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u3, v, y[j], 0, 0, 0);
+                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v, y[j], 0, 0, 0);
+                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v, y[j], 0, 0, 0);
+                            } else {
+                                // a float16 value is two bf16 parts, exactly
+                                float h[8];
+#pragma unroll
+                                for (int q = 0; q < 8; ++q)
+                                    h[q] = from16<IGEMM_F16>((uint16_t)(w[q / 2] >> (16 * (q & 1))));
+                                v8bf v1, v2, v3;
+                                split3(h, v1, v2, v3);
+                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v2, y[j], 0, 0, 0);
+                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u3, v1, y[j], 0, 0, 0);
+                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v2, y[j], 0, 0, 0);
+                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v1, y[j], 0, 0, 0);
+                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v1, y[j], 0, 0, 0);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4) {
+                        const int4 id = *(const int4 *)(arow_id + r0 + M::out_row(lane, r));
+                        const int ids[4] = {id.x, id.y, id.z, id.w};
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int j = 0; j < TN; ++j)
+                                x[j][r + q] = ids[q] == which ? x[j][r + q] + y[j][r + q]
+                                                              : x[j][r + q];
+                    }
+                }
+            }
+            constexpr int P = WN * ES + 16;  // (the pad keeps four rows off one bank)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    put<T>(blk + M::out_row(lane, r) * P, 32 * j + M::out_col(lane), x[j][r]);
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            const int c = (lane % LPR) * V, col = n0 + wn0 + c;
+#pragma unroll
+            for (int q = 0; q < 32; q += 64 / LPR) {
+                const int lr = q + lane / LPR;
+                const int o = orow[r0 + lr];
+                if (o < 0) continue;
+                const char *src = blk + lr * P + c * ES;
+                char *dst = (char *)p.out + ((int64_t)o * p.ldo + col) * ES;
+                if (col + V <= p.n) {
+                    const v4i v = *(const v4i *)src;
+                    __builtin_memcpy(dst, &v, 16);
+                } else {
+                    for (int e = 0; col + e < p.n; ++e)
+                        if constexpr (ES == 4) ((float *)dst)[e] = ((const float *)src)[e];
+                        else ((uint16_t *)dst)[e] = ((const uint16_t *)src)[e];
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+    if (p.type == IGEMM_F32) emit(ic<IGEMM_F32>{});
+    else if (p.type == IGEMM_BF16) emit(ic<IGEMM_BF16>{});
+    else emit(ic<IGEMM_F16>{});
+}
+
+}  // namespace rows
+}  // namespace igemm
