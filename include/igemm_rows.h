@@ -70,7 +70,7 @@ typedef enum igemm_type {
  * top_groups or group_best out of their ranges (top_k <= experts, groups a
  * divisor of experts, 1 <= top_groups <= groups), ld < experts, or a scale
  * that is not finite; IGEMM_ENOTSUP for more than 1024 experts, top_k or groups
- * over 64, or tokens * top_k beyond 2^31 - 1. tokens = 0 writes offsets alone.
+ * over 64, or tokens * top_k beyond 2^31 - 2^16. tokens = 0 writes offsets alone.
  */
 #define IGEMM_SOFTMAX 0
 #define IGEMM_SIGMOID 1
@@ -146,7 +146,7 @@ int igemm_i8_grouped(const igemm_grouped_desc *desc, const int32_t *offsets,
  *   out      tokens x n, ldo >= n; overwritten; overlaps neither Z nor, unless
  *            it is the same, base.
  * Errors: IGEMM_EINVAL as for igemm_i16 (top_k >= 1); IGEMM_ENOTSUP for n, tokens
- * or top_k beyond 2^31 - 1. tokens = 0 or n = 0: IGEMM_OK.
+ * or top_k beyond 2^31 - 1 or a grid beyond 2^31 - 1 workgroups. tokens = 0 or n = 0: IGEMM_OK.
  */
 int igemm_combine(int64_t tokens, int64_t top_k, int64_t n, int type, const void *Z, int64_t ldz,
                   const float *weights, const int32_t *ids, const void *base, int64_t ld_base,

@@ -1,9 +1,18 @@
 // Routing of tokens to experts, and the plan of the experts' products.
 //
-// One wave a token. Scores and keys are formed in 64-bit floating point: with
-// 32 bits about one token in a few thousand has an expert within rounding of
-// the border of the chosen ones, and which side it falls on would depend on
-// the order of the softmax's sum.
+// A wave a token, expert e = 64 v + lane in register v. The top_k largest keys
+// are found by their bits: a threshold is built from the highest bit down, a
+// ballot and a population count telling how many keys reach it, and the search
+// ends as soon as that is top_k (some 20 steps of a compare a register and scalar
+// work, where top_k rounds of a maximum over the wave take six exchanges each).
+// The chosen then move to the first lanes, where each counts the ones before it.
+//
+// Keys are compared as 64-bit floating point: with 32 bits about one token in a
+// few thousand has an expert within rounding of the border of the chosen ones,
+// and which side it falls on would depend on the order of the softmax's sum.
+// Where the keys are in the order of the logits (no bias, and one group or groups
+// by their best), the logits' 32 bits are compared instead, and exp is taken of
+// the chosen ones alone.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -13,199 +22,493 @@ namespace igemm {
 namespace rows {
 namespace {
 
-constexpr double kNone = -__builtin_huge_val();
-
-// The largest key of the wave and its index (the lower one of equals); index -1
-// if every key is kNone.
-__device__ __forceinline__ void wave_best(double &key, int &idx) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const double k = __shfl_xor(key, d);
-        const int i = __shfl_xor(idx, d);
-        const bool take = k > key || (k == key && (unsigned)i < (unsigned)idx);
-        key = take ? k : key;
-        idx = take ? i : idx;
-    }
+// Unsigned integers in the order of the floating point numbers, all above 0,
+// which stands for an excluded expert. (-0 is made +0 by the callers.)
+__device__ __forceinline__ u32 ordered(float x) {
+    const u32 b = __builtin_bit_cast(u32, x);
+    return b >> 31 ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ uint64_t ordered(double x) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    return b >> 63 ? ~b : b | 0x8000000000000000ull;
+}
+__device__ __forceinline__ double unordered(uint64_t k) {
+    return __builtin_bit_cast(double, k >> 63 ? k & 0x7fffffffffffffffull : ~k);
+}
+__device__ __forceinline__ double read_lane(double x, int l) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const u32 lo = (u32)__builtin_amdgcn_readlane((int)(u32)b, l);
+    const u32 hi = (u32)__builtin_amdgcn_readlane((int)(u32)(b >> 32), l);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ uint64_t read_lane(uint64_t x, int l) {
+    return __builtin_bit_cast(uint64_t, read_lane(__builtin_bit_cast(double, x), l));
+}
+__device__ __forceinline__ u32 read_lane(u32 x, int l) {
+    return (u32)__builtin_amdgcn_readlane((int)x, l);
+}
+__device__ __forceinline__ int below_me(uint64_t mask) {
+    return __builtin_amdgcn_mbcnt_hi((u32)(mask >> 32), __builtin_amdgcn_mbcnt_lo((u32)mask, 0));
 }
 
-// Expert e = 64 v + lane in register v.
-template <int V, int T>
-__global__ void __launch_bounds__(64)
-route_tokens(igemm_route_desc d, const void *__restrict__ logits, int64_t ld,
-             const float *__restrict__ bias, int32_t *__restrict__ ids,
-             float *__restrict__ weights) {
-    const int64_t t = blockIdx.x;
-    const int lane = threadIdx.x;
-    __shared__ double key_s[64 * V];
+template <bool WIDE>
+struct KeyOf {
+    typedef u32 type;
+};
+template <>
+struct KeyOf<true> {
+    typedef uint64_t type;
+};
+
+// A wave's LDS: the keys by expert (groups), then the chosen ones.
+template <int V, bool WIDE>
+struct Scratch {
+    typename KeyOf<WIDE>::type key[64 * V];
+    typename KeyOf<WIDE>::type best[64];
+    float logit[64];
+    int index[64];
+};
+
+// LDS written by lanes of a wave and read by others of the same wave.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+template <int V, int T, bool WIDE>
+__device__ void route_token(const igemm_route_desc &d, int64_t t, const void *__restrict__ logits,
+                            int64_t ld, const float *__restrict__ bias, int32_t *__restrict__ ids,
+                            float *__restrict__ weights, Scratch<V, WIDE> &sc) {
+    typedef typename KeyOf<WIDE>::type key_t;
+    constexpr int BITS = sizeof(key_t) * 8;
+    const float none = -__builtin_huge_valf();
+    const int lane = threadIdx.x & 63;
     float l[V];
-    double s[V], key[V];
-    float top = -__builtin_huge_valf();
+    key_t key[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int e = 64 * v + lane;
-        l[v] = e < d.experts ? get<T>(logits, t * ld + e) : -__builtin_huge_valf();
-        l[v] = l[v] == l[v] ? fminf(l[v], 3.402823466e38f) : -__builtin_huge_valf();
-        top = fmaxf(top, l[v]);
+        const float x = e < d.experts ? get<T>(logits, t * ld + e) : none;
+        // (x + 0: no -0)
+        l[v] = x == x ? fminf(x, 3.402823466e38f) + 0.0f : none;
     }
-    // (exp and the sigmoid lose the order of logits that are far apart or large)
-    const bool by_logit = bias == nullptr && (d.groups == 1 || d.group_best == 1);
+    const bool all = WIDE || !d.renormalise;  // every expert's score is needed
+    float top = 0.0f;
     double total = 1.0;
-    if (d.score == IGEMM_SOFTMAX) {
+    if (all && d.score == IGEMM_SOFTMAX) {
+        top = none;
+#pragma unroll
+        for (int v = 0; v < V; ++v) top = fmaxf(top, l[v]);
+#pragma unroll
         for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
         total = 0.0;
     }
+    auto score = [&](float x) -> double {  // before the division by total
+        return d.score == IGEMM_SOFTMAX ? exp((double)x - (double)top)
+                                        : 1.0 / (1.0 + exp(-(double)x));
+    };
+    if constexpr (WIDE) {
+        double s[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const bool in = l[v] > -__builtin_huge_valf();
-        if (d.score == IGEMM_SOFTMAX) {
-            s[v] = in ? exp((double)l[v] - (double)top) : 0.0;
-            total += s[v];
-        } else {
-            s[v] = in ? 1.0 / (1.0 + exp(-(double)l[v])) : 0.0;
+        for (int v = 0; v < V; ++v) {
+            s[v] = l[v] > none ? score(l[v]) : 0.0;
+            if (d.score == IGEMM_SOFTMAX) total += s[v];
         }
-    }
-    if (d.score == IGEMM_SOFTMAX) {
-        for (int x = 32; x > 0; x /= 2) total += __shfl_xor(total, x);
-        if (total == 0.0) total = 1.0;
-    }
+        if (d.score == IGEMM_SOFTMAX) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int e = 64 * v + lane;
-        const bool in = l[v] > -__builtin_huge_valf();
-        s[v] /= total;
-        key[v] = !in ? kNone : by_logit ? (double)l[v] : s[v] + (bias != nullptr ? (double)bias[e] : 0.0);
-        if (!(key[v] == key[v])) key[v] = kNone;
+            for (int x = 32; x > 0; x /= 2) total += __shfl_xor(total, x);
+            if (total == 0.0) total = 1.0;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const double k =
+                s[v] / total + (bias != nullptr && l[v] > none ? (double)bias[64 * v + lane] : 0.0);
+            key[v] = l[v] > none && k > -__builtin_huge_val() ? ordered(k + 0.0) : 0;
+        }
+    } else {
+        if (all && d.score == IGEMM_SOFTMAX) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) total += l[v] > none ? score(l[v]) : 0.0;
+#pragma unroll
+            for (int x = 32; x > 0; x /= 2) total += __shfl_xor(total, x);
+            if (total == 0.0) total = 1.0;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = l[v] > none ? ordered(l[v]) : 0;
     }
+
+    // ---- groups -----------------------------------------------------------------
     if (d.groups > 1) {
         const int size = d.experts / d.groups;
+        int per = 1, lg = 0;  // lanes a group: a power of two
+        while (2 * per * d.groups <= 64) per *= 2, ++lg;
 #pragma unroll
-        for (int v = 0; v < V; ++v) key_s[64 * v + lane] = key[v];
-        __syncthreads();
-        // lane g: its group's best one or two
-        double a = kNone, b = kNone;
-        if (lane < d.groups)
-            for (int e = lane * size; e < (lane + 1) * size; ++e) {
-                const double x = key_s[e];
-                if (x > a) {
-                    b = a;
-                    a = x;
-                } else if (x > b) {
-                    b = x;
-                }
+        for (int v = 0; v < V; ++v) sc.key[64 * v + lane] = key[v];
+        wave_sync();
+        const int g = lane >> lg, sub = lane & (per - 1);
+        key_t a = 0, b = 0;  // the best two
+        if (g < d.groups)
+            for (int e = sub; e < size; e += per) {
+                const key_t x = sc.key[g * size + e];
+                b = x > a ? a : (x > b ? x : b);
+                a = x > a ? x : a;
             }
-        double score = d.group_best == 2 && b > kNone ? a + b : a;
-        uint64_t kept = 0;
-        for (int c = 0; c < d.top_groups; ++c) {
-            double k = score;
-            int i = k > kNone ? lane : -1;
-            wave_best(k, i);
-            if (i < 0) break;
-            kept |= 1ull << i;
-            if (lane == i) score = kNone;
+        for (int x = 1; x < per; x *= 2) {
+            const key_t oa = __shfl_xor(a, x), ob = __shfl_xor(b, x);
+            const key_t lo = a < oa ? a : oa;
+            a = a < oa ? oa : a;
+            b = b < ob ? ob : b;
+            b = b < lo ? lo : b;
         }
+        key_t mine = a;
+        if constexpr (WIDE) {
+            if (d.group_best == 2 && b != 0) mine = ordered(unordered(a) + unordered(b) + 0.0);
+        }
+        int rank = 0;
+        for (int x = 0; x < d.groups; ++x) {
+            const key_t other = read_lane(mine, x << lg);
+            rank += other > mine || (other == mine && x < g);
+        }
+        // bit x << lg: group x stays
+        const uint64_t kept = __ballot(g < d.groups && mine != 0 && rank < d.top_groups);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (!((kept >> ((64 * v + lane) / size & 63)) & 1)) key[v] = kNone;
+        for (int v = 0; v < V; ++v) {
+            const int x = min((64 * v + lane) / size, d.groups - 1);
+            if (!((kept >> (x << lg)) & 1)) key[v] = 0;
+        }
     }
-    double mine = 0.0, sum = 0.0;
-    int id = -1;
-    for (int c = 0; c < d.top_k; ++c) {
-        double k = kNone, sc = 0.0;
-        int i = -1;
+
+    // ---- the top_k --------------------------------------------------------------
+    auto reach = [&](key_t th) -> int {
+        int c = 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (key[v] > k) {
-                k = key[v];
-                i = 64 * v + lane;
-                sc = s[v];
+        for (int v = 0; v < V; ++v) c += __popcll(__ballot(key[v] >= th));
+        return c;
+    };
+    const int k = min(d.top_k, reach(1));
+    key_t th = 0;
+    if (k > 0) {
+        for (int b = BITS - 1; b >= 0; --b) {
+            const key_t next = th | ((key_t)1 << b);
+            const int c = reach(next);
+            if (c >= k) th = next;
+            if (c == k) break;
+        }
+    }
+    // keys above th, and of those equal to it the first ones that still fit
+    int room = k;
+#pragma unroll
+    for (int v = 0; v < V; ++v) room -= __popcll(__ballot(key[v] > th));
+    int base = 0;
+    if (k > 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint64_t equal = __ballot(key[v] == th);
+            const bool in = key[v] > th || (key[v] == th && below_me(equal) < room);
+            room -= min(room, __popcll(equal));
+            const uint64_t mask = __ballot(in);
+            if (in) {
+                const int at = base + below_me(mask);
+                sc.best[at] = key[v];
+                sc.logit[at] = l[v];
+                sc.index[at] = 64 * v + lane;
             }
-        const int own = i;
-        wave_best(k, i);
-        if (i < 0) break;
-        sc = __shfl(own == i ? sc : 0.0, i & 63);
-        sum += sc;
-        if (lane == c) {
-            mine = sc;
-            id = i;
+            base += __popcll(mask);
         }
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (64 * v + lane == i) key[v] = kNone;
     }
+    wave_sync();
+    // The chosen are in the order of their index: of equals the first comes first.
+    const bool mine = lane < k;
+    const key_t best = mine ? sc.best[lane] : 0;
+    const float x = mine ? sc.logit[lane] : none;
+    const int index = mine ? sc.index[lane] : -1;
+    if (!all && d.score == IGEMM_SOFTMAX) {
+        top = x;  // the largest logit is among the chosen
+#pragma unroll
+        for (int o = 32; o > 0; o /= 2) top = fmaxf(top, __shfl_xor(top, o));
+    }
+    const double s = mine ? score(x) / total : 0.0;
+    int rank = 0;
+    double sum = 0.0;
+    for (int j = 0; j < k; ++j) {
+        const key_t other = read_lane(best, j);
+        rank += other > best || (other == best && j < lane);
+        sum += read_lane(s, j);
+    }
+    double w = s;
+    if (d.renormalise) w = sum > 0.0 ? s / sum : 0.0;
     if (lane < d.top_k) {
-        double w = mine;
-        if (d.renormalise) w = sum > 0.0 ? w / sum : 0.0;
-        ids[t * d.top_k + lane] = id;
-        weights[t * d.top_k + lane] = (float)(w * (double)d.scale);
+        const int at = mine ? rank : lane;
+        ids[t * d.top_k + at] = index;
+        weights[t * d.top_k + at] = mine ? (float)(w * (double)d.scale) : 0.0f;
+    }
+    wave_sync();  // (the scratch is the next token's)
+}
+
+// ---- the plan -------------------------------------------------------------------
+//
+// The slots of [s0, s1) into order, a run of consecutive slots a wave: the waves
+// count their slots of each expert, the counts become each wave's first place,
+// and each wave then takes its slots 64 at a time, in order; lanes of the same
+// expert find each other by one ballot for each bit of the index. start[e]: the
+// place of this range's first slot of expert e.
+template <int WAVES>
+__device__ void place_slots(const int32_t *ids, int s0, int s1, int experts, int *start,
+                            int *count /* WAVES x experts */, int32_t *order) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int e = tid; e < WAVES * experts; e += WAVES * 64) count[e] = 0;
+    __syncthreads();
+    const int run = ((s1 - s0 + WAVES - 1) / WAVES + 63) / 64 * 64;
+    const int w0 = s0 + wave * run, w1 = min(w0 + run, s1);
+    for (int s = w0 + lane; s < w1; s += 64) {
+        const int id = ids[s];
+        if (id >= 0) atomicAdd(&count[wave * experts + id], 1);
+    }
+    __syncthreads();
+    for (int e = tid; e < experts; e += WAVES * 64) {
+        int at = start[e];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const int c = count[w * experts + e];
+            count[w * experts + e] = at;
+            at += c;
+        }
+    }
+    __syncthreads();
+    const int bits = 32 - __clz(experts);  // (ids and experts itself, for none)
+    for (int s = w0; s < w1; s += 64) {
+        const int id = s + lane < w1 ? ids[s + lane] : -1;
+        const int x = id >= 0 ? id : experts;
+        uint64_t same = ~0ull;
+        for (int b = 0; b < bits; ++b) {
+            const bool on = (x >> b) & 1;
+            const uint64_t m = __ballot(on);
+            same &= on ? m : ~m;
+        }
+        if (id >= 0) {
+            const int rank = below_me(same);
+            const int at = count[wave * experts + id];
+            order[at + rank] = s + lane;
+        }
+        wave_sync();
+        if (id >= 0 && below_me(same) == 0) count[wave * experts + id] += __popcll(same);
+        wave_sync();
     }
 }
 
-// One workgroup an expert: where it begins, and its slots in order.
-__global__ void __launch_bounds__(256)
-plan_plain(const int32_t *__restrict__ ids, int slots, int experts, int32_t *__restrict__ offsets,
-           int32_t *__restrict__ order) {
-    const int e = blockIdx.x, tid = threadIdx.x;   // e == experts: the end
-    __shared__ int cnt[256];
-    int below = 0;
-    for (int s = tid; s < slots; s += 256) below += ids[s] >= 0 && ids[s] < e;
-    cnt[tid] = below;
-    __syncthreads();
-    for (int d = 128; d > 0; d /= 2) {
-        if (tid < d) cnt[tid] += cnt[tid + d];
-        __syncthreads();
-    }
-    int at = cnt[0];
-    __syncthreads();
-    if (tid == 0) offsets[e] = at;
-    if (e == experts) {
-        for (int s = at + tid; s < slots; s += 256) order[s] = -1;
-        return;
-    }
-    for (int s0 = 0; s0 < slots; s0 += 256) {
-        const bool mine = s0 + tid < slots && ids[s0 + tid] == e;
-        cnt[tid] = mine;
-        __syncthreads();
-        for (int d = 1; d < 256; d *= 2) {
-            const int x = tid >= d ? cnt[tid - d] : 0;
-            __syncthreads();
-            cnt[tid] += x;
-            __syncthreads();
+// Exclusive sums of value[0 .. n), n <= 1024, in place; returns their total.
+template <int WAVES>
+__device__ int scan_experts(int *value, int n, int *waves /* WAVES */) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int carry = 0;
+    for (int e0 = 0; e0 < n; e0 += WAVES * 64) {
+        const int v = e0 + tid < n ? value[e0 + tid] : 0;
+        int sum = v;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int up = __shfl_up(sum, o);
+            if (lane >= o) sum += up;
         }
-        if (mine) order[at + cnt[tid] - 1] = s0 + tid;
-        at += cnt[255];
+        if (lane == 63) waves[wave] = sum;
+        __syncthreads();
+        int before = carry;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            if (w < wave) before += waves[w];
+            carry += waves[w];
+        }
+        if (e0 + tid < n) value[e0 + tid] = before + sum - v;
         __syncthreads();
     }
+    return carry;
+}
+
+// The whole plan by one workgroup.
+template <int WAVES>
+__device__ void plan_alone(const int32_t *ids, int slots, int experts, int32_t *offsets,
+                           int32_t *order, int *start, int *count, int *waves) {
+    const int tid = threadIdx.x;
+    for (int e = tid; e < experts; e += WAVES * 64) start[e] = 0;
+    __syncthreads();
+    for (int s = tid; s < slots; s += WAVES * 64)
+        if (ids[s] >= 0) atomicAdd(&start[ids[s]], 1);
+    __syncthreads();
+    const int total = scan_experts<WAVES>(start, experts, waves);
+    for (int e = tid; e < experts; e += WAVES * 64) offsets[e] = start[e];
+    if (tid == 0) offsets[experts] = total;
+    for (int s = total + tid; s < slots; s += WAVES * 64) order[s] = -1;
+    place_slots<WAVES>(ids, 0, slots, experts, start, count, order);
+}
+
+// ---- kernels ----------------------------------------------------------------------
+
+template <int V, int T, bool WIDE>
+__global__ void __launch_bounds__(256)
+route_tokens(igemm_route_desc d, const void *__restrict__ logits, int64_t ld,
+             const float *__restrict__ bias, int32_t *ids, float *weights) {
+    __shared__ Scratch<V, WIDE> sc[4];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t t = (int64_t)blockIdx.x * 4 + wave;
+    if (t < d.tokens) route_token<V, T, WIDE>(d, t, logits, ld, bias, ids, weights, sc[wave]);
+}
+
+// A few tokens: one workgroup routes them, a wave each, and makes the plan.
+constexpr int kFewWaves = 16, kFewExperts = 256;
+template <int V, int T, bool WIDE>
+__global__ void __launch_bounds__(kFewWaves * 64)
+route_few(igemm_route_desc d, const void *__restrict__ logits, int64_t ld,
+          const float *__restrict__ bias, int32_t *ids, float *weights, int32_t *offsets,
+          int32_t *order) {
+    __shared__ union {
+        Scratch<V, WIDE> sc[kFewWaves];
+        int count[kFewWaves * 64 * V];
+    } m;
+    __shared__ int start[64 * V], waves[kFewWaves];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int t = wave; t < d.tokens; t += kFewWaves)
+        route_token<V, T, WIDE>(d, t, logits, ld, bias, ids, weights, m.sc[wave]);
+    __syncthreads();
+    plan_alone<kFewWaves>(ids, (int)d.tokens * d.top_k, d.experts, offsets, order, start, m.count,
+                          waves);
+}
+
+constexpr int kPlanWaves = 16;
+__global__ void __launch_bounds__(kPlanWaves * 64)
+plan_one(const int32_t *ids, int slots, int experts, int32_t *offsets, int32_t *order) {
+    __shared__ int start[1024], waves[kPlanWaves];
+    __shared__ int count[kPlanWaves * 1024];
+    plan_alone<kPlanWaves>(ids, slots, experts, offsets, order, start, count, waves);
+}
+
+// Many slots: `chunk` of them a workgroup, whose counts of each expert go to
+// counts[block][expert]; then each workgroup places its own after those of the
+// experts and workgroups before.
+__global__ void __launch_bounds__(256)
+plan_counts(const int32_t *__restrict__ ids, int slots, int experts, int chunk,
+            int32_t *__restrict__ counts) {
+    __shared__ int start[1024];
+    const int tid = threadIdx.x;
+    for (int e = tid; e < experts; e += 256) start[e] = 0;
+    __syncthreads();
+    const int64_t s0 = (int64_t)blockIdx.x * chunk;
+    const int64_t s1 = min(s0 + chunk, (int64_t)slots);
+    for (int64_t s = s0 + tid; s < s1; s += 256)
+        if (ids[s] >= 0) atomicAdd(&start[ids[s]], 1);
+    __syncthreads();
+    for (int e = tid; e < experts; e += 256) counts[blockIdx.x * experts + e] = start[e];
+}
+__global__ void __launch_bounds__(kPlanWaves * 64)
+plan_places(const int32_t *__restrict__ ids, int slots, int experts, int chunk,
+            const int32_t *__restrict__ counts, int32_t *__restrict__ offsets,
+            int32_t *__restrict__ order) {
+    __shared__ int start[1024], before[1024], waves[kPlanWaves];
+    __shared__ int count[kPlanWaves * 1024];
+    const int tid = threadIdx.x, blocks = gridDim.x;
+    for (int e = tid; e < experts; e += kPlanWaves * 64) {
+        int mine = 0, all = 0;
+#pragma unroll 8
+        for (int b = 0; b < blocks; ++b) {
+            const int c = counts[b * experts + e];
+            mine += b < (int)blockIdx.x ? c : 0;
+            all += c;
+        }
+        start[e] = all;
+        before[e] = mine;
+    }
+    __syncthreads();
+    const int total = scan_experts<kPlanWaves>(start, experts, waves);
+    if (blockIdx.x == 0) {
+        for (int e = tid; e < experts; e += kPlanWaves * 64) offsets[e] = start[e];
+        if (tid == 0) offsets[experts] = total;
+    }
+    __syncthreads();
+    for (int e = tid; e < experts; e += kPlanWaves * 64) start[e] += before[e];
+    const int64_t s0 = (int64_t)blockIdx.x * chunk;
+    const int64_t s1 = min(s0 + chunk, (int64_t)slots);
+    for (int64_t s = max((int64_t)total, s0) + tid; s < s1; s += kPlanWaves * 64) order[s] = -1;
+    __syncthreads();
+    place_slots<kPlanWaves>(ids, (int)s0, (int)s1, experts, start, count, order);
 }
 
 template <int V>
-const void *pick(int type) {
-    return type == IGEMM_F32    ? (const void *)route_tokens<V, IGEMM_F32>
-           : type == IGEMM_BF16 ? (const void *)route_tokens<V, IGEMM_BF16>
-                                : (const void *)route_tokens<V, IGEMM_F16>;
+const void *pick(int type, bool wide) {
+    if (wide)
+        return type == IGEMM_F32    ? (const void *)route_tokens<V, IGEMM_F32, true>
+               : type == IGEMM_BF16 ? (const void *)route_tokens<V, IGEMM_BF16, true>
+                                    : (const void *)route_tokens<V, IGEMM_F16, true>;
+    return type == IGEMM_F32    ? (const void *)route_tokens<V, IGEMM_F32, false>
+           : type == IGEMM_BF16 ? (const void *)route_tokens<V, IGEMM_BF16, false>
+                                : (const void *)route_tokens<V, IGEMM_F16, false>;
+}
+template <int V>
+const void *pick_few(int type, bool wide) {
+    if (wide)
+        return type == IGEMM_F32    ? (const void *)route_few<V, IGEMM_F32, true>
+               : type == IGEMM_BF16 ? (const void *)route_few<V, IGEMM_BF16, true>
+                                    : (const void *)route_few<V, IGEMM_F16, true>;
+    return type == IGEMM_F32    ? (const void *)route_few<V, IGEMM_F32, false>
+           : type == IGEMM_BF16 ? (const void *)route_few<V, IGEMM_BF16, false>
+                                : (const void *)route_few<V, IGEMM_F16, false>;
+}
+
+// One workgroup places up to this many slots; more are cut into at most kMostBlocks
+// ranges.
+constexpr int64_t kAlone = 8192, kChunk = 2048, kMostBlocks = 128;
+int64_t chunk_of(int64_t slots) {
+    const int64_t c = (slots + kMostBlocks - 1) / kMostBlocks;
+    return c > kChunk ? c : kChunk;
 }
 
 }  // namespace
 
-int64_t route_workspace(const igemm_route_desc &d, bool plan) { return 0; }
+int64_t route_workspace(const igemm_route_desc &d, bool plan) {
+    const int64_t slots = d.tokens * d.top_k;
+    if (!plan || slots <= kAlone) return 0;
+    const int64_t chunk = chunk_of(slots);
+    return ((slots + chunk - 1) / chunk * d.experts * 4 + 255) / 256 * 256;
+}
 
 int launch_route(const igemm_route_desc &d, const void *logits, int64_t ld, const float *bias,
                  int32_t *ids, float *weights, int32_t *offsets, int32_t *order, void *workspace,
                  void *stream_) {
     hipStream_t stream = (hipStream_t)stream_;
+    const bool wide = bias != nullptr || (d.groups > 1 && d.group_best == 2);
+    igemm_route_desc dd = d;
+    const int slots = (int)(d.tokens * d.top_k);
+    if (offsets != nullptr && d.tokens > 0 && d.tokens <= 2 * kFewWaves &&
+        d.experts <= kFewExperts) {
+        const void *fn = d.experts <= 64    ? pick_few<1>(d.type, wide)
+                         : d.experts <= 128 ? pick_few<2>(d.type, wide)
+                                            : pick_few<4>(d.type, wide);
+        void *args[] = {&dd,  (void *)&logits, &ld, (void *)&bias, &ids, &weights, &offsets,
+                        &order};
+        return hipLaunchKernel(fn, dim3(1), dim3(kFewWaves * 64), args, 0, stream) == hipSuccess
+                   ? IGEMM_OK
+                   : IGEMM_EHIP;
+    }
     if (d.tokens > 0) {
-        const void *fn = d.experts <= 64    ? pick<1>(d.type)
-                         : d.experts <= 128 ? pick<2>(d.type)
-                         : d.experts <= 256 ? pick<4>(d.type)
-                         : d.experts <= 512 ? pick<8>(d.type)
-                                            : pick<16>(d.type);
-        igemm_route_desc dd = d;
+        const void *fn = d.experts <= 64    ? pick<1>(d.type, wide)
+                         : d.experts <= 128 ? pick<2>(d.type, wide)
+                         : d.experts <= 256 ? pick<4>(d.type, wide)
+                         : d.experts <= 512 ? pick<8>(d.type, wide)
+                                            : pick<16>(d.type, wide);
         void *args[] = {&dd, (void *)&logits, &ld, (void *)&bias, &ids, &weights};
-        if (hipLaunchKernel(fn, dim3((unsigned)d.tokens), dim3(64), args, 0, stream) != hipSuccess)
+        if (hipLaunchKernel(fn, dim3((unsigned)((d.tokens + 3) / 4)), dim3(256), args, 0,
+                            stream) != hipSuccess)
             return IGEMM_EHIP;
     }
-    if (offsets != nullptr)
-        plan_plain<<<dim3((unsigned)d.experts + 1), 256, 0, stream>>>(
-            ids, (int)(d.tokens * d.top_k), d.experts, offsets, order);
+    if (offsets == nullptr) return IGEMM_OK;
+    if (slots <= kAlone) {
+        plan_one<<<dim3(1), kPlanWaves * 64, 0, stream>>>(ids, slots, d.experts, offsets, order);
+    } else {
+        const int chunk = (int)chunk_of(slots);
+        const unsigned blocks = (unsigned)(((int64_t)slots + chunk - 1) / chunk);
+        int32_t *counts = (int32_t *)workspace;
+        plan_counts<<<dim3(blocks), 256, 0, stream>>>(ids, slots, d.experts, chunk, counts);
+        plan_places<<<dim3(blocks), kPlanWaves * 64, 0, stream>>>(ids, slots, d.experts, chunk,
+                                                                  counts, offsets, order);
+    }
     return hipGetLastError() == hipSuccess ? IGEMM_OK : IGEMM_EHIP;
 }
 

@@ -46,7 +46,7 @@ int check_route(const igemm_route_desc *d) {
         (d->score != IGEMM_SOFTMAX && d->score != IGEMM_SIGMOID) ||
         (d->renormalise != 0 && d->renormalise != 1) || !isfinite(d->scale) || !type_ok(d->type))
         return IGEMM_EINVAL;
-    if (d->experts > 1024 || d->top_k > 64 || d->groups > 64 || d->tokens > kMax / d->top_k)
+    if (d->experts > 1024 || d->top_k > 64 || d->groups > 64 || d->tokens > (kMax - 65535) / d->top_k)
         return IGEMM_ENOTSUP;
     return IGEMM_OK;
 }
