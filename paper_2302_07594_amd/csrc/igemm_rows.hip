@@ -102,7 +102,6 @@ shrink_tiles(Product p, Adapters ad, float *__restrict__ u, int rpad) {
         v16f acc;
 #pragma unroll
         for (int q = 0; q < 16; ++q) acc[q] = 0.0f;
-#pragma unroll 4
         for (int k0 = kb; k0 < ke; k0 += 32) {
             // 32 k in two instructions: lane half h holds k 16 h .. 16 h + 15 of
             // both operands, eight at a time.
@@ -206,20 +205,76 @@ join_slices(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpa
 
 // ---- the sum of a token's slots ---------------------------------------------------
 
-template <int T>
+// One pass over Z. A thread takes 16 bytes of a row, eight slots' loads at a time
+// before the first is used; a group of `lanes` threads (a power of two) covers a
+// row, or 16 * lanes bytes of it. Slots left out read the token's first slot's
+// row instead, which is at hand, so that no load waits for an id's branch.
+template <int T, bool WAVE>
 __global__ void __launch_bounds__(256)
-combine_plain(int64_t tokens, int top_k, int n, const void *Z, int64_t ldz, const float *weights,
-              const int32_t *ids, const void *base, int64_t ld_base, void *out, int64_t ldo) {
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < tokens * n;
-         e += (int64_t)gridDim.x * 256) {
-        const int64_t t = e / n;
-        const int c = (int)(e - t * n);
-        float x = base != nullptr ? get<T>(base, t * ld_base + c) : 0.0f;
-        for (int j = 0; j < top_k; ++j) {
-            const int64_t s = t * top_k + j;
-            if (ids == nullptr || ids[s] >= 0) x += weights[s] * get<T>(Z, s * ldz + c);
+combine_slots(int64_t tokens, int top_k, int n, const char *Z, int64_t ldz,
+              const float *__restrict__ weights, const int32_t *__restrict__ ids,
+              const char *base, int64_t ld_base, char *out, int64_t ldo, int lanes,
+              int pieces) {
+    constexpr int ES = T == IGEMM_F32 ? 4 : 2, V = 16 / ES;
+    const int tid = threadIdx.x, per = (int)blockDim.x / lanes;
+    const u32 at = blockIdx.x * per + tid / lanes, row = at / (u32)pieces;
+    int64_t t = row;
+    const int c = ((int)(at - row * (u32)pieces) * lanes + tid % lanes) * V;
+    if constexpr (WAVE)  // the whole wave has one token: its weights are scalars
+        t = (int64_t)__builtin_amdgcn_readfirstlane((int)t);
+    if (t >= tokens || c >= n) return;
+    const bool whole = c + V <= n;
+    auto fetch = [&](const char *row) -> v4i {
+        if (whole) return ring::load_u16(row + (int64_t)c * ES);
+        return load_elems<ES == 4 ? 1 : 2>(row + (int64_t)c * ES, 0, ES == 4 ? (n - c) * 4 : n - c);
+    };
+    auto value = [&](v4i v, int e) -> float {
+        const int word = v[ES == 4 ? e : e / 2];
+        if constexpr (ES == 4) return __builtin_bit_cast(float, word);
+        else return from16<T>((uint16_t)((u32)word >> (16 * (e & 1))));
+    };
+    float x[V] = {};
+    if (base != nullptr) {
+        const v4i b = fetch(base + t * ld_base * ES);
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[e] = value(b, e);
+    }
+    const int64_t s0 = t * top_k;
+    for (int j0 = 0; j0 < top_k; j0 += 8) {
+        v4i z[8];
+        float w[8];
+        bool on[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool in = j0 + j < top_k;
+            const int64_t s = s0 + (in ? j0 + j : 0);
+            on[j] = in && (ids == nullptr || ids[s] >= 0);
+            w[j] = weights[s];
         }
-        put<T>(out, t * ldo + c, x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            z[j] = fetch(Z + (on[j] ? s0 + j0 + j : s0) * ldz * ES);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] = on[j] ? fmaf(w[j], value(z[j], e), x[e]) : x[e];
+    }
+    char *dst = out + (t * ldo + c) * ES;
+    if (whole) {
+        v4i r;
+        if constexpr (ES == 4) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = __builtin_bit_cast(int, x[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                r[e] = (int)((u32)to16<T>(x[2 * e]) | (u32)to16<T>(x[2 * e + 1]) << 16);
+        }
+        __builtin_memcpy(dst, &r, 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (c + e < n) put<T>(dst, e, x[e]);
     }
 }
 
@@ -340,18 +395,28 @@ int launch_combine(int64_t tokens, int64_t top_k, int64_t n, int type, const voi
                    const float *weights, const int32_t *ids, const void *base, int64_t ld_base,
                    void *out, int64_t ldo, void *stream_) {
     hipStream_t stream = (hipStream_t)stream_;
-    const int64_t blocks = (tokens * n + 255) / 256;
-    const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192));
-    if (type == IGEMM_F32)
-        combine_plain<IGEMM_F32><<<grid, 256, 0, stream>>>(tokens, (int)top_k, (int)n, Z, ldz, weights,
-                                                           ids, base, ld_base, out, ldo);
-    else if (type == IGEMM_BF16)
-        combine_plain<IGEMM_BF16><<<grid, 256, 0, stream>>>(tokens, (int)top_k, (int)n, Z, ldz,
-                                                            weights, ids, base, ld_base, out, ldo);
-    else
-        combine_plain<IGEMM_F16><<<grid, 256, 0, stream>>>(tokens, (int)top_k, (int)n, Z, ldz,
-                                                           weights, ids, base, ld_base, out, ldo);
-    return hipGetLastError() == hipSuccess ? IGEMM_OK : IGEMM_EHIP;
+    const int vec = type == IGEMM_F32 ? 4 : 8;
+    // Few values: workgroups of one wave, so that more compute units share them.
+    const int threads = tokens * n >= (int64_t)num_cu_of_current_device() * 4 * 256 * vec ? 256 : 64;
+    int lanes = 1;
+    while (lanes < threads && (int64_t)lanes * vec < n) lanes *= 2;
+    int pieces = (int)((n + (int64_t)lanes * vec - 1) / ((int64_t)lanes * vec));
+    const int64_t per = threads / lanes, blocks = (tokens * pieces + per - 1) / per;
+    if (tokens * pieces > 0x7fffffff) return IGEMM_ENOTSUP;
+    const bool wave = lanes >= 64;
+#define IGEMM_COMBINE(t)                                           \
+    (wave ? (const void *)combine_slots<t, true> : (const void *)combine_slots<t, false>)
+    const void *fn = type == IGEMM_F32    ? IGEMM_COMBINE(IGEMM_F32)
+                     : type == IGEMM_BF16 ? IGEMM_COMBINE(IGEMM_BF16)
+                                          : IGEMM_COMBINE(IGEMM_F16);
+#undef IGEMM_COMBINE
+    int ki = (int)top_k, ni = (int)n;
+    void *args[] = {&tokens, &ki,  &ni, (void *)&Z, &ldz,   (void *)&weights, (void *)&ids,
+                    (void *)&base, &ld_base, &out,  &ldo, &lanes, &pieces};
+    return hipLaunchKernel(fn, dim3((unsigned)blocks), dim3((unsigned)threads), args, 0, stream) ==
+                   hipSuccess
+               ? IGEMM_OK
+               : IGEMM_EHIP;
 }
 
 }  // namespace rows
