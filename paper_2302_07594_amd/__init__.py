@@ -972,6 +972,14 @@ def route(logits, top_k, bias=None, groups=1, top_groups=1, group_best=1, score=
     id -1 and weight 0 where no expert is left, and the plan that grouped_i8
     takes, int32 (experts + 1) and (tokens * top_k); plan=False leaves the plan
     out (None, None). workspace as for gemm_i16 (None or a uint8 tensor)."""
+    if stream is None and workspace is None and score in ("softmax", "sigmoid"):
+        r = (_native or _load_native()).route(
+            logits, top_k, bias, groups, top_groups, group_best, 1 if score == "sigmoid" else 0,
+            1 if renormalise else 0, scale, 1 if plan else 0)
+        if r is not None:
+            if not isinstance(r, tuple):
+                raise IgemmError(r, "route")
+            return r
     import torch
     f = (torch.float32, torch.bfloat16, torch.float16)
     ld = _expect("route", "logits", logits, f, (None, None), None)
@@ -1013,6 +1021,14 @@ def grouped_i8(A, B, offsets, order=None, scale_a=None, scale_b=None, slots=0, s
     out: (out_rows, n) float32, bfloat16 or float16 with unit stride along rows,
     overwritten where a position leads; None: a zeroed (rows, n) tensor of out_dtype
     (default bfloat16). Returns out. Raises IgemmError on a bad status."""
+    if out is not None and out_dtype is None and rows is None and stream is None and \
+            workspace is None:
+        st = (_native or _load_native()).grouped(A, B, offsets, order, scale_a, scale_b, slots,
+                                                 1 if scatter else 0, out)
+        if st is not None:
+            if st != IGEMM_OK:
+                raise IgemmError(st, "grouped_i8")
+            return out
     import torch
     i8, i32, f32 = (torch.int8,), (torch.int32,), (torch.float32,)
     lda = _expect("grouped_i8", "A", A, i8, (None, None), None)
@@ -1057,6 +1073,12 @@ def combine(Z, weights, ids=None, base=None, out=None, stream=None):
     stride along rows; weights: float32 (tokens, top_k), contiguous; ids: int32 of
     that shape or None; base and out: (tokens, n) of Z's type (out may be base; None:
     a new tensor). Returns out."""
+    if out is not None and stream is None:
+        st = (_native or _load_native()).combine(Z, weights, ids, base, out)
+        if st is not None:
+            if st != IGEMM_OK:
+                raise IgemmError(st, "combine")
+            return out
     import torch
     f = (torch.float32, torch.bfloat16, torch.float16)
     _expect("combine", "weights", weights, (torch.float32,), (None, None), None, rows=False)
@@ -1094,6 +1116,13 @@ def adapters_i8(A, B, ids=None, down=None, up=None, scale_a=None, scale_b=None, 
     None. ids, down and up are given together; without them: the projection alone.
     out: (m, n) float32, bfloat16 or float16 with unit stride along rows; None: a new
     tensor of out_dtype (default bfloat16). Returns out."""
+    if out is not None and out_dtype is None and stream is None and workspace is None:
+        st = (_native or _load_native()).adapters(A, B, ids, down, up, scale_a, scale_b, ranks,
+                                                  scaling, out)
+        if st is not None:
+            if st != IGEMM_OK:
+                raise IgemmError(st, "adapters_i8")
+            return out
     import torch
     i8, i32, f32 = (torch.int8,), (torch.int32,), (torch.float32,)
     name = "adapters_i8"

@@ -20,6 +20,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "igemm.h"
+#include "igemm_rows.h"
 
 namespace {
 
@@ -262,11 +263,249 @@ PyObject *conv2d(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- products whose rows choose their weights --------------------------------------
+
+// None, or a plain tensor: *t stays null for None.
+bool plain_or_none(PyObject *o, at::ScalarType dt, int64_t dim, const at::Tensor **t) {
+    *t = nullptr;
+    if (o == Py_None) return true;
+    *t = plain(o, dt, dim);
+    return *t != nullptr;
+}
+// A plain float, bfloat16 or half tensor; its igemm_type in *type.
+const at::Tensor *plain_real(PyObject *o, int64_t dim, int *type) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::ScalarType dt = THPVariable_Unpack(o).scalar_type();
+    if (dt == at::kFloat) *type = IGEMM_F32;
+    else if (dt == at::kBFloat16) *type = IGEMM_BF16;
+    else if (dt == at::kHalf) *type = IGEMM_F16;
+    else return nullptr;
+    return plain(o, dt, dim);
+}
+// A dense tensor of one or two dimensions of these extents (null: fine).
+bool dense(const at::Tensor *t, int64_t d0, int64_t d1 = -1) {
+    return t == nullptr || (t->is_contiguous() && t->size(0) == d0 &&
+                            (d1 < 0 || t->size(1) == d1));
+}
+// The stream of the current device if all tensors (some may be null) live there.
+bool all_here(std::initializer_list<const at::Tensor *> ts, void **stream) {
+    const auto s = c10::hip::getCurrentHIPStreamMasqueradingAsCUDA();
+    for (const at::Tensor *t : ts)
+        if (t != nullptr && t->device() != s.device()) return false;
+    *stream = (void *)s.stream();
+    return true;
+}
+template <class T>
+T *data(const at::Tensor *t) {
+    return t != nullptr ? (T *)t->data_ptr() : nullptr;
+}
+// Strides of a stack of matrices with unit stride along rows.
+bool stacked(const at::Tensor &t, int64_t *ld, int64_t *stride) {
+    if (t.size(2) > 1 && t.stride(2) != 1) return false;
+    *ld = t.size(1) > 1 ? t.stride(1) : (t.size(2) > 1 ? t.size(2) : 1);
+    *stride = t.size(0) > 1 ? t.stride(0) : 0;
+    return true;
+}
+PyObject *status(int st) { return PyLong_FromLong(st); }
+
+// route(logits, top_k, bias, groups, top_groups, group_best, sigmoid, renormalise, scale,
+//       plan) -> None, a status, or (ids, weights, offsets, order)
+PyObject *route(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    igemm_route_desc d;
+    int sigmoid, renormalise, plan, st;
+    void *stream;
+    const at::Tensor *l = nargs == 10 ? plain_real(args[0], 2, &d.type) : nullptr, *bias;
+    int64_t ld;
+    if (!l || modes_active() || !as_int(args[1], &d.top_k) ||
+        !plain_or_none(args[2], at::kFloat, 1, &bias) || !as_int(args[3], &d.groups) ||
+        !as_int(args[4], &d.top_groups) || !as_int(args[5], &d.group_best) ||
+        !as_int(args[6], &sigmoid) || !as_int(args[7], &renormalise) ||
+        !PyFloat_Check(args[8]) || !as_int(args[9], &plan) || l->numel() == 0 ||
+        l->size(1) > INT_MAX || !leading(*l, &ld) || !dense(bias, l->size(1)) ||
+        !all_here({l, bias}, &stream))
+        Py_RETURN_NONE;
+    d.tokens = l->size(0);
+    d.experts = (int)l->size(1);
+    d.score = sigmoid ? IGEMM_SIGMOID : IGEMM_SOFTMAX;
+    d.renormalise = renormalise;
+    d.scale = (float)PyFloat_AS_DOUBLE(args[8]);
+    at::Tensor ids, weights, offsets, order;
+    {
+        pybind11::gil_scoped_release no_gil;
+        int64_t wb = 0;
+        st = igemm_route_query(&d, &wb);
+        if (st == IGEMM_OK) {
+            const auto ints = l->options().dtype(at::kInt);
+            ids = at::empty({d.tokens, d.top_k}, ints);
+            weights = at::empty({d.tokens, d.top_k}, l->options().dtype(at::kFloat));
+            if (plan) {
+                offsets = at::empty({d.experts + 1}, ints);
+                order = at::empty({d.tokens * d.top_k}, ints);
+            }
+            at::Tensor ws;
+            void *wp = nullptr;
+            if (plan && wb > 0) ws = workspace(*l, wb, &wp);
+            st = igemm_route(&d, l->data_ptr(), ld, data<float>(bias), (int32_t *)ids.data_ptr(),
+                             (float *)weights.data_ptr(),
+                             plan ? (int32_t *)offsets.data_ptr() : nullptr,
+                             plan ? (int32_t *)order.data_ptr() : nullptr, wp, wp ? wb : 0,
+                             stream);
+        }
+    }
+    if (st != IGEMM_OK) return status(st);
+    PyObject *r = PyTuple_New(4);
+    if (r == nullptr) return nullptr;
+    PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(std::move(ids)));
+    PyTuple_SET_ITEM(r, 1, THPVariable_Wrap(std::move(weights)));
+    for (int i = 0; i < 2; ++i) {
+        PyObject *o = Py_None;
+        if (plan) o = THPVariable_Wrap(std::move(i == 0 ? offsets : order));
+        else Py_INCREF(o);
+        PyTuple_SET_ITEM(r, 2 + i, o);
+    }
+    for (int i = 0; i < 4; ++i)
+        if (PyTuple_GET_ITEM(r, i) == nullptr) {
+            Py_DECREF(r);
+            return nullptr;
+        }
+    return r;
+    END_HANDLE_TH_ERRORS
+}
+
+// grouped(A, B, offsets, order, scale_a, scale_b, slots, scatter, out) -> None or a status
+PyObject *grouped(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    if (nargs != 9) Py_RETURN_NONE;
+    igemm_grouped_desc d;
+    const at::Tensor *a = plain(args[0], at::kChar, 2);
+    const at::Tensor *b = a ? plain(args[1], at::kChar, 3) : nullptr;
+    const at::Tensor *off = b ? plain(args[2], at::kInt, 1) : nullptr;
+    const at::Tensor *out = off ? plain_real(args[8], 2, &d.type) : nullptr, *order, *sa, *sb;
+    int64_t lda, ldb, ldo, stride_b;
+    int st;
+    void *stream;
+    if (!out || modes_active() || !plain_or_none(args[3], at::kInt, 1, &order) ||
+        !plain_or_none(args[4], at::kFloat, 1, &sa) ||
+        !plain_or_none(args[5], at::kFloat, 2, &sb) || !as_i64(args[6], &d.slots) ||
+        !as_int(args[7], &d.scatter) || a->numel() == 0 || b->numel() == 0 || out->numel() == 0)
+        Py_RETURN_NONE;
+    d.a_rows = a->size(0);
+    d.k = a->size(1);
+    d.groups = b->size(0);
+    d.n = b->size(2);
+    d.out_rows = out->size(0);
+    d.rows = order ? order->size(0) : d.a_rows;
+    if (b->size(1) != d.k || out->size(1) != d.n || !dense(off, d.groups + 1) ||
+        !dense(order, d.rows) || !dense(sa, d.a_rows) || !dense(sb, d.groups, d.n) ||
+        !leading(*a, &lda) || !stacked(*b, &ldb, &stride_b) || !leading(*out, &ldo) ||
+        !all_here({a, b, off, order, sa, sb, out}, &stream))
+        Py_RETURN_NONE;
+    {
+        pybind11::gil_scoped_release no_gil;
+        int64_t wb = 0;
+        st = igemm_i8_grouped_query(&d, num_cu(*a), &wb);
+        at::Tensor ws;
+        void *wp = nullptr;
+        if (st == IGEMM_OK && wb > 0) ws = workspace(*a, wb, &wp);
+        if (st == IGEMM_OK)
+            st = igemm_i8_grouped(&d, data<int32_t>(off), data<int32_t>(order), data<int8_t>(a),
+                                  lda, data<float>(sa), data<int8_t>(b), ldb, stride_b,
+                                  data<float>(sb), out->data_ptr(), ldo, wp, wb, stream);
+    }
+    return status(st);
+    END_HANDLE_TH_ERRORS
+}
+
+// combine(Z, weights, ids, base, out) -> None or a status
+PyObject *combine(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    int type, st;
+    const at::Tensor *z = nargs == 5 ? plain_real(args[0], 2, &type) : nullptr;
+    const at::Tensor *w = z ? plain(args[1], at::kFloat, 2) : nullptr, *ids, *base;
+    const at::Tensor *out = w ? plain(args[4], z->scalar_type(), 2) : nullptr;
+    int64_t ldz, ld_base = 0, ldo;
+    void *stream;
+    if (!out || modes_active() || !plain_or_none(args[2], at::kInt, 2, &ids) ||
+        !plain_or_none(args[3], z->scalar_type(), 2, &base) || z->numel() == 0)
+        Py_RETURN_NONE;
+    const int64_t tokens = w->size(0), top_k = w->size(1), n = z->size(1);
+    if (z->size(0) != tokens * top_k || !dense(w, tokens, top_k) || !dense(ids, tokens, top_k) ||
+        out->size(0) != tokens || out->size(1) != n ||
+        (base && (base->size(0) != tokens || base->size(1) != n || !leading(*base, &ld_base))) ||
+        !leading(*z, &ldz) || !leading(*out, &ldo) || !all_here({z, w, ids, base, out}, &stream))
+        Py_RETURN_NONE;
+    {
+        pybind11::gil_scoped_release no_gil;
+        st = igemm_combine(tokens, top_k, n, type, z->data_ptr(), ldz, data<float>(w),
+                           data<int32_t>(ids), data<void>(base), ld_base, out->data_ptr(), ldo,
+                           stream);
+    }
+    return status(st);
+    END_HANDLE_TH_ERRORS
+}
+
+// adapters(A, B, ids, down, up, scale_a, scale_b, ranks, scaling, out) -> None or a status
+PyObject *adapters(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    if (nargs != 10) Py_RETURN_NONE;
+    igemm_adapters_desc d;
+    const at::Tensor *a = plain(args[0], at::kChar, 2);
+    const at::Tensor *b = a ? plain(args[1], at::kChar, 2) : nullptr;
+    const at::Tensor *ids = b ? plain(args[2], at::kInt, 1) : nullptr;
+    const at::Tensor *down = ids ? plain_real(args[3], 3, &d.weight_type) : nullptr;
+    const at::Tensor *up = down ? plain(args[4], down->scalar_type(), 3) : nullptr;
+    const at::Tensor *out = up ? plain_real(args[9], 2, &d.type) : nullptr;
+    const at::Tensor *sa, *sb, *ranks, *scaling;
+    int64_t lda, ldb, ldo, ldd, ldu, stride_d, stride_u;
+    int st;
+    void *stream;
+    if (!out || modes_active() || d.weight_type == IGEMM_F32 ||
+        !plain_or_none(args[5], at::kFloat, 1, &sa) ||
+        !plain_or_none(args[6], at::kFloat, 1, &sb) ||
+        !plain_or_none(args[7], at::kInt, 1, &ranks) ||
+        !plain_or_none(args[8], at::kFloat, 1, &scaling) || a->numel() == 0 || b->numel() == 0 ||
+        down->numel() == 0 || up->numel() == 0)
+        Py_RETURN_NONE;
+    d.m = a->size(0);
+    d.k = a->size(1);
+    d.n = b->size(1);
+    d.adapters = down->size(0);
+    d.rank = down->size(1);
+    if (b->size(0) != d.k || down->size(2) != d.k || up->size(0) != d.adapters ||
+        up->size(1) != d.n || up->size(2) != d.rank || out->size(0) != d.m ||
+        out->size(1) != d.n || !dense(ids, d.m) || !dense(sa, d.m) || !dense(sb, d.n) ||
+        !dense(ranks, d.adapters) || !dense(scaling, d.adapters) || !leading(*a, &lda) ||
+        !leading(*b, &ldb) || !stacked(*down, &ldd, &stride_d) ||
+        !stacked(*up, &ldu, &stride_u) || !leading(*out, &ldo) ||
+        !all_here({a, b, ids, down, up, sa, sb, ranks, scaling, out}, &stream))
+        Py_RETURN_NONE;
+    {
+        pybind11::gil_scoped_release no_gil;
+        int64_t wb = 0;
+        st = igemm_i8_adapters_query(&d, num_cu(*a), &wb);
+        at::Tensor ws;
+        void *wp = nullptr;
+        if (st == IGEMM_OK && wb > 0) ws = workspace(*a, wb, &wp);
+        if (st == IGEMM_OK)
+            st = igemm_i8_adapters(&d, data<int8_t>(a), lda, data<float>(sa), data<int8_t>(b), ldb,
+                                   data<float>(sb), data<int32_t>(ids), down->data_ptr(), ldd,
+                                   stride_d, up->data_ptr(), ldu, stride_u, data<int32_t>(ranks),
+                                   data<float>(scaling), out->data_ptr(), ldo, wp, wb, stream);
+    }
+    return status(st);
+    END_HANDLE_TH_ERRORS
+}
+
 #define IGEMM_FAST(f) (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr
 PyMethodDef methods[] = {{"gemm", IGEMM_FAST(gemm)},
                          {"srs", IGEMM_FAST(srs)},
                          {"packed_b", IGEMM_FAST(packed_b)},
                          {"conv2d", IGEMM_FAST(conv2d)},
+                         {"route", IGEMM_FAST(route)},
+                         {"grouped", IGEMM_FAST(grouped)},
+                         {"combine", IGEMM_FAST(combine)},
+                         {"adapters", IGEMM_FAST(adapters)},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_igemm_torch", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -613,3 +613,30 @@ def test_refusals_leave_the_output_alone():
         ig.route(torch.zeros(2, 4, device="cuda"), 5)
     torch.cuda.synchronize()
     assert bool((out == 7).all())
+
+
+def test_plain_calls_take_the_compiled_binding(monkeypatch):
+    """What the Python code would do is the same, and plain calls do not reach it."""
+    layer = Layer(40)
+    k = {}
+    layer(keep=k)
+    a, off, order = k["x"], k["offsets"], k["order"]
+    out = torch.zeros(120, 256, dtype=BF16, device="cuda")  # (the padded token has no rows)
+    y = torch.empty(40, 192, dtype=BF16, device="cuda")
+    calls = [
+        lambda **kw: ig.route(k["logits"], 3, **kw),
+        lambda **kw: ig.grouped_i8(a, layer.w1, off, order, k["s"], layer.s1, slots=3, out=out,
+                                   **kw),
+        lambda **kw: ig.combine(k["z"], k["w"], ids=k["ids"], base=k["base"], out=y, **kw),
+        lambda **kw: ig.adapters_i8(a, layer.w0, layer.ids, layer.down, layer.up, k["s"],
+                                    layer.s0, out=y, **kw)]
+    copy = lambda r: tuple(t.clone() for t in (r if isinstance(r, tuple) else (r,)))  # noqa: E731
+    slow = [copy(f(stream=torch.cuda.current_stream())) for f in calls]
+
+    def refuse(*a, **kw):
+        raise AssertionError("the Python path ran")
+    monkeypatch.setattr(ig, "_on", refuse)
+    for f, want in zip(calls, slow):
+        assert all(torch.equal(g, w) for g, w in zip(copy(f()), want))
+    with pytest.raises(ig.IgemmError):
+        ig.route(k["logits"], 10)
