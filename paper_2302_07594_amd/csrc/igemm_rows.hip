@@ -21,57 +21,11 @@ __device__ __forceinline__ v4i load_row16(const int8_t *row, int e0, int len) {
 }
 
 // ---- u = scaling scale_a A down^T -------------------------------------------------
-//
-// Few rows, or few ranks: a workgroup a row and k slice, every wave one rank in
-// four at a time, 16 bytes of `down` a lane. What it reads of `down` is one
-// adapter a row, whichever the row's is, so a batch of 16 requests with an
-// adapter each takes as long as one with a shared adapter.
-constexpr int kShrinkK = 1024;  // k a workgroup: two passes of 64 lanes x 8
 
-template <int T>
+// Few rows or few ranks, where the product is not sliced (shrink_row).
 __global__ void __launch_bounds__(256)
 shrink_rows(Product p, Adapters ad, float *__restrict__ u, int rpad) {
-    const int i = blockIdx.x, z = blockIdx.y;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int which = ad.ids[i];
-    const int rank = rank_of(ad, which);
-    if (rank == 0) return;
-    const int8_t *a = p.A + (int64_t)i * p.lda;
-    constexpr int PASS = kShrinkK / 512;
-    float x[PASS][8];
-#pragma unroll
-    for (int q = 0; q < PASS; ++q) {
-        const int e0 = z * kShrinkK + 512 * q + 8 * lane;
-        u32 w[2] = {0u, 0u};
-        if (e0 + 8 <= p.k) {
-            __builtin_memcpy(w, a + e0, 8);
-        } else {
-            for (int e = 0; e < 8 && e0 + e < p.k; ++e)
-                w[e >> 2] |= (u32)(uint8_t)a[e0 + e] << (8 * (e & 3));
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[q][e] = (float)byte_of(w[e >> 2], e & 3);
-    }
-    float f = p.scale_a != nullptr ? p.scale_a[i] : 1.0f;
-    if (ad.scaling != nullptr) f *= ad.scaling[which];
-    const uint16_t *down = (const uint16_t *)ad.down + which * ad.stride_down;
-    for (int r = wave; r < rank; r += 4) {
-        const uint16_t *d = down + r * ad.ld_down;
-        float s = 0.0f;
-#pragma unroll
-        for (int q = 0; q < PASS; ++q) {
-            const int e0 = z * kShrinkK + 512 * q + 8 * lane;
-            if (e0 >= p.k) continue;
-            u32 w[4];
-            load8(d, e0, p.k, p.k, w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                s = fmaf(x[q][e], from16<T>((uint16_t)(w[e / 2] >> (16 * (e & 1)))), s);
-        }
-#pragma unroll
-        for (int o = 32; o > 0; o /= 2) s += __shfl_xor(s, o);
-        if (lane == 0) u[((int64_t)z * p.rows + i) * rpad + r] = s * f;
-    }
+    shrink_row<4>(p, ad, u, rpad, blockIdx.x, blockIdx.y);
 }
 
 // Many rows: 32 rows x 32 ranks a workgroup on the matrix cores, k over its eight
@@ -102,32 +56,53 @@ shrink_tiles(Product p, Adapters ad, float *__restrict__ u, int rpad) {
         v16f acc;
 #pragma unroll
         for (int q = 0; q < 16; ++q) acc[q] = 0.0f;
-        for (int k0 = kb; k0 < ke; k0 += 32) {
-            // 32 k in two instructions: lane half h holds k 16 h .. 16 h + 15 of
-            // both operands, eight at a time.
-            const int e0 = k0 + 16 * half;
-            const v4i av = load_row16(a, e0, p.k);
+        // 32 k in two instructions: lane half h holds k 16 h .. 16 h + 15 of both
+        // operands, eight at a time.
+        auto step = [&](v4i av, const v4i (&dv)[2]) __attribute__((always_inline)) {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                u32 w[4];
-                load8(d, e0 + 8 * q, p.k, p.k, w);
-                const v4u w4 = {w[0], w[1], w[2], w[3]};
                 if constexpr (T == IGEMM_BF16) {
                     v8bf x;
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         x[e] = (__bf16)(float)byte_of((u32)av[2 * q + e / 4], e & 3);
                     acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        x, __builtin_bit_cast(v8bf, w4), acc, 0, 0, 0);
+                        x, __builtin_bit_cast(v8bf, dv[q]), acc, 0, 0, 0);
                 } else {
                     v8h x;
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         x[e] = (_Float16)(float)byte_of((u32)av[2 * q + e / 4], e & 3);
                     acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                        x, __builtin_bit_cast(v8h, w4), acc, 0, 0, 0);
+                        x, __builtin_bit_cast(v8h, dv[q]), acc, 0, 0, 0);
                 }
             }
+        };
+        // Four steps' loads before the first is used; the last k apart, bounded.
+        int k0 = kb;
+        constexpr int AHEAD = 4;
+        for (; k0 + 32 * AHEAD <= ke; k0 += 32 * AHEAD) {
+            v4i av[AHEAD], dv[AHEAD][2];
+#pragma unroll
+            for (int x = 0; x < AHEAD; ++x) {
+                const int e0 = k0 + 32 * x + 16 * half;
+                av[x] = ring::load_u16((const char *)a + e0);
+                dv[x][0] = ring::load_u16((const char *)(d + e0));
+                dv[x][1] = ring::load_u16((const char *)(d + e0 + 8));
+            }
+#pragma unroll
+            for (int x = 0; x < AHEAD; ++x) step(av[x], dv[x]);
+        }
+        for (; k0 < ke; k0 += 32) {
+            const int e0 = k0 + 16 * half;
+            v4i dv[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                u32 w[4];
+                load8(d, e0 + 8 * q, p.k, p.k, w);
+                dv[q] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+            }
+            step(load_row16(a, e0, p.k), dv);
         }
         __syncthreads();
 #pragma unroll
@@ -157,6 +132,11 @@ join_slices(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpa
     __shared__ float us[1024];
     const int i = blockIdx.y, lane = threadIdx.x & 63;
     const int c = blockIdx.x * 256 + threadIdx.x;
+    int sum = 0;
+    if (c < p.n) {
+#pragma unroll 8
+        for (int z = 0; z < slices; ++z) sum += part[((int64_t)z * p.rows + i) * p.n + c];
+    }
     int g = 0;
     if (p.offsets != nullptr) {
         int below = 0;
@@ -181,8 +161,6 @@ join_slices(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpa
         __syncthreads();
     }
     if (c >= p.n) return;
-    int sum = 0;
-    for (int z = 0; z < slices; ++z) sum += part[((int64_t)z * p.rows + i) * p.n + c];
     float x = (float)sum * (p.scale_a != nullptr ? p.scale_a[a] : 1.0f);
     if (p.scale_b != nullptr) x *= p.scale_b[(int64_t)g * p.n + c];
     if (rank > 0) {
@@ -281,7 +259,7 @@ combine_slots(int64_t tokens, int top_k, int n, const char *Z, int64_t ldz,
 // ---- choices --------------------------------------------------------------------------
 
 struct Choice {
-    int bm;           // rows of a tile; 128 columns
+    int bm, bn;       // tile
     int slices, kchunk;
     bool by_row;      // u: a workgroup a row (ks k slices), else 32 x 32 blocks
     int ks, rpad;
@@ -289,31 +267,47 @@ struct Choice {
 };
 
 int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // By sizes alone, so that the workspace can be sized before the operands exist.
+// What the device will find is taken to be even: `used` groups of `avg` rows.
 Choice choose(int64_t rows, int64_t n, int64_t k, int64_t groups, int64_t adapters, int64_t rank,
               int num_cu) {
     Choice c = {};
-    const int64_t used = groups < rows ? groups : rows;   // groups that may have rows
-    const int64_t avg = (rows + used - 1) / used;
-    c.bm = avg <= 32 ? 32 : avg <= 64 ? 64 : 128;
-    const int64_t tiles = (avg + c.bm - 1) / c.bm * used * ((n + 127) / 128);
+    const int64_t used = groups < rows ? groups : rows;
+    const int64_t avg = ceil_div(rows, used);
+    auto tiles = [&](int64_t bm, int64_t bn) { return ceil_div(avg, bm) * used * ceil_div(n, bn); };
+    // share of the last round of workgroups (`at` at a time) that has work
+    auto full = [](int64_t t, int64_t at) { return (double)t / (double)(ceil_div(t, at) * at); };
+    if (avg <= 32) {
+        c.bm = 32, c.bn = 256;
+    } else if (avg <= 64 || tiles(128, 128) < num_cu) {
+        c.bm = 64, c.bn = 256;
+    } else if (avg >= 192 &&
+               full(tiles(256, 256), num_cu) >= 0.9 * full(tiles(128, 128), 2 * num_cu)) {
+        c.bm = 256, c.bn = 256;
+    } else {
+        c.bm = 128, c.bn = 128;
+    }
+    // Fewer tiles than compute units: narrower ones, then k slices.
     int64_t slices = 1;
-    if (2 * tiles <= num_cu) {
-        slices = num_cu / tiles;
+    if (c.bm <= 64 && tiles(c.bm, 256) < num_cu) {
+        c.bn = 128;
+        const int64_t t = tiles(c.bm, 128);
+        if (2 * t <= num_cu) slices = num_cu / t;
         if (slices > k / 256) slices = k / 256;
         if (slices > 16) slices = 16;
         if (slices < 1) slices = 1;
     }
-    int64_t chunk = ((k + slices - 1) / slices + kStepK - 1) / kStepK * kStepK;
+    int64_t chunk = ceil_div(ceil_div(k, slices), kStepK) * kStepK;
     if (chunk < kStepK) chunk = kStepK;
     c.kchunk = (int)chunk;
-    c.slices = k > 0 ? (int)((k + chunk - 1) / chunk) : 1;
+    c.slices = k > 0 ? (int)ceil_div(k, chunk) : 1;
     if (c.slices > 1) c.part_bytes = up256(c.slices * rows * n * 4);
     if (adapters > 0 && rank > 0) {
-        c.rpad = (int)((rank + 15) / 16 * 16);
-        c.by_row = rows * rank <= 4096;
-        c.ks = c.by_row ? (int)((k + kShrinkK - 1) / kShrinkK) : 1;
+        c.rpad = (int)(ceil_div(rank, 16) * 16);
+        c.by_row = c.slices > 1 || rows * rank <= 4096;
+        c.ks = c.by_row ? (int)ceil_div(k, kShrinkK) : 1;
         c.u_bytes = up256(c.ks * rows * c.rpad * 4);
     }
     return c;
@@ -325,15 +319,35 @@ int64_t most_tiles(int64_t rows, int64_t groups, int64_t bm) {
     return (rows + used * (bm - 1)) / bm;
 }
 
-template <int BM, int WM, int WN, int NST, int OCC>
-const void *pick(bool reg, bool part, bool adapt) {
+template <int BM, int BN, int WM, int WN, int NST, int OCC, bool REG>
+const void *pick_epi(bool part, bool adapt) {
+    if (part) {
+        if constexpr (BM <= 64 && BN == 128)
+            return adapt ? (const void *)rows_tile<BM, BN, WM, WN, NST, OCC, REG, true, true>
+                         : (const void *)rows_tile<BM, BN, WM, WN, NST, OCC, REG, true, false>;
+        return nullptr;
+    }
+    return adapt ? (const void *)rows_tile<BM, BN, WM, WN, NST, OCC, REG, false, true>
+                 : (const void *)rows_tile<BM, BN, WM, WN, NST, OCC, REG, false, false>;
+}
+// The tile's kernel and its threads. (us, random operands that are not cached:
+// 64 rows of 64 experts, 1024 x 2048: 32 x 256 20.5, 32 x 128 23.5; 4096 rows,
+// 2048 x 1024: 64 x 256 41.9, 64 x 128 42.4, 128 x 128 47.9; 32768 rows, 4096 x 2048:
+// 256 x 256 358, 128 x 256 404, 128 x 128 442; one weight, 8192 x 11008 x 4096: 351,
+// 377, 391; 2048 x 4096 x 4096, 128 tiles of 256 x 256: 53, else 38.)
+const void *pick(int bm, int bn, bool reg, bool part, bool adapt, int *threads) {
+    *threads = bm == 256 || (bm == 64 && bn == 256 && !reg) ? 512 : 256;
     if (reg)
-        return part    ? (const void *)rows_tile<BM, 128, WM, WN, 2, OCC, true, true, false>
-               : adapt ? (const void *)rows_tile<BM, 128, WM, WN, 2, OCC, true, false, true>
-                       : (const void *)rows_tile<BM, 128, WM, WN, 2, OCC, true, false, false>;
-    return part    ? (const void *)rows_tile<BM, 128, WM, WN, NST, OCC, false, true, false>
-           : adapt ? (const void *)rows_tile<BM, 128, WM, WN, NST, OCC, false, false, true>
-                   : (const void *)rows_tile<BM, 128, WM, WN, NST, OCC, false, false, false>;
+        return bm == 32    ? (bn == 256 ? pick_epi<32, 256, 32, 64, 2, 2, true>(part, adapt)
+                                        : pick_epi<32, 128, 32, 32, 2, 2, true>(part, adapt))
+               : bm == 64  ? pick_epi<64, 128, 32, 64, 2, 2, true>(part, adapt)
+                           : pick_epi<128, 128, 64, 64, 2, 2, true>(part, adapt);
+    return bm == 32    ? (bn == 256 ? pick_epi<32, 256, 32, 64, 4, 1, false>(part, adapt)
+                                    : pick_epi<32, 128, 32, 32, 3, 2, false>(part, adapt))
+           : bm == 64  ? (bn == 256 ? pick_epi<64, 256, 32, 64, 3, 1, false>(part, adapt)
+                                    : pick_epi<64, 128, 32, 64, 3, 2, false>(part, adapt))
+           : bm == 128 ? pick_epi<128, 128, 64, 64, 2, 2, false>(part, adapt)
+                       : pick_epi<256, 256, 128, 64, 2, 1, false>(part, adapt);
 }
 
 }  // namespace
@@ -350,16 +364,24 @@ int launch_product(const Product &p, const Adapters &ad, int num_cu, void *works
     const Choice c = choose(p.rows, p.n, p.k, p.groups, ad.adapters, ad.rank, num_cu);
     int32_t *part = (int32_t *)workspace;
     float *u = (float *)((char *)workspace + c.part_bytes);
-    const int tiles_n = (p.n + 127) / 128;
-    const int64_t grid = most_tiles(p.rows, p.groups, c.bm) * tiles_n * c.slices;
-    if (grid > 0x7fffffff) return IGEMM_ENOTSUP;
-    if (ad.adapters > 0) {
+    const bool sliced = c.slices > 1, adapt = ad.adapters > 0;
+    // By DMA where rows start at 4-byte addresses and the offsets of a whole last
+    // k-tile stay below 4 GiB; else through registers, in tiles that have the
+    // registers for it.
+    const bool reg = (uintptr_t)p.A % 4 != 0 || (uintptr_t)p.B % 4 != 0 || p.lda % 4 != 0 ||
+                     p.ldb % 4 != 0 || p.stride_b % 4 != 0 ||
+                     ((int64_t)p.k + kStepK) * p.ldb > 0xffffffffll;
+    int bm = c.bm, bn = c.bn, threads = 0;
+    if (reg && bm >= 64) bn = 128;
+    if (reg && bm == 256) bm = 128;
+    const void *fn = pick(bm, bn, reg, sliced, adapt, &threads);
+    const int64_t first = sliced && adapt ? (int64_t)p.rows * c.ks : 0;
+    const int64_t grid = first + most_tiles(p.rows, p.groups, bm) * ceil_div(p.n, bn) * c.slices;
+    if (fn == nullptr || grid > 0x7fffffff) return IGEMM_ENOTSUP;
+    if (adapt && !sliced) {
         if (c.by_row) {
             const dim3 g((unsigned)p.rows, (unsigned)c.ks);
-            if (ad.type == IGEMM_BF16)
-                shrink_rows<IGEMM_BF16><<<g, 256, 0, stream>>>(p, ad, u, c.rpad);
-            else
-                shrink_rows<IGEMM_F16><<<g, 256, 0, stream>>>(p, ad, u, c.rpad);
+            shrink_rows<<<g, 256, 0, stream>>>(p, ad, u, c.rpad);
         } else {
             const dim3 g((unsigned)((p.rows + 31) / 32), (unsigned)((ad.rank + 31) / 32));
             if (ad.type == IGEMM_BF16)
@@ -369,21 +391,12 @@ int launch_product(const Product &p, const Adapters &ad, int num_cu, void *works
         }
         if (hipGetLastError() != hipSuccess) return IGEMM_EHIP;
     }
-    // By DMA where rows start at 4-byte addresses and the offsets of a whole last
-    // k-tile stay below 4 GiB.
-    const bool reg = (uintptr_t)p.A % 4 != 0 || (uintptr_t)p.B % 4 != 0 || p.lda % 4 != 0 ||
-                     p.ldb % 4 != 0 || p.stride_b % 4 != 0 ||
-                     ((int64_t)p.k + kStepK) * p.ldb > 0xffffffffll;
-    const bool sliced = c.slices > 1, adapt = ad.adapters > 0 && !sliced;
-    const void *fn = c.bm == 32   ? pick<32, 32, 32, 3, 2>(reg, sliced, adapt)
-                     : c.bm == 64 ? pick<64, 32, 64, 3, 2>(reg, sliced, adapt)
-                                  : pick<128, 64, 64, 2, 2>(reg, sliced, adapt);
     Product pp = p;
     Adapters aa = ad;
-    const float *uc = u;
     int ks = c.ks, rpad = c.rpad, slices = c.slices, kchunk = c.kchunk;
-    void *args[] = {&pp, &aa, &uc, &ks, &rpad, &part, &slices, &kchunk};
-    if (hipLaunchKernel(fn, dim3((unsigned)grid), dim3(256), args, 0, stream) != hipSuccess)
+    void *args[] = {&pp, &aa, &u, &ks, &rpad, &part, &slices, &kchunk};
+    if (hipLaunchKernel(fn, dim3((unsigned)grid), dim3((unsigned)threads), args, 0, stream) !=
+        hipSuccess)
         return IGEMM_EHIP;
     if (sliced)
         join_slices<<<dim3((unsigned)((p.n + 255) / 256), (unsigned)p.rows), 256, 0, stream>>>(

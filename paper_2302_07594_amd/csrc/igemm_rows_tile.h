@@ -78,13 +78,84 @@ __device__ __forceinline__ int rank_of(const Adapters &ad, int which) {
     return ad.ranks != nullptr ? min(max(ad.ranks[which], 0), ad.rank) : ad.rank;
 }
 
+// u = scaling scale_a A down^T for few rows or few ranks: row i and k slice z by
+// one workgroup, every wave a rank in WAVES at a time, 16 bytes of `down` a lane.
+// What it reads of `down` is one adapter a row, whichever the row's is, so a
+// batch of 16 requests with an adapter each takes as long as one with a shared
+// one.
+constexpr int kShrinkK = 1024;  // k a workgroup: two passes of 64 lanes x 8
+template <int WAVES>
+__device__ void shrink_row(const Product &p, const Adapters &ad, float *__restrict__ u, int rpad,
+                           int i, int z) {
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int which = ad.ids[i];
+    const int rank = rank_of(ad, which);
+    if (rank == 0) return;
+    const int8_t *a = p.A + (int64_t)i * p.lda;
+    constexpr int PASS = kShrinkK / 512;
+    float x[PASS][8];
+#pragma unroll
+    for (int q = 0; q < PASS; ++q) {
+        const int e0 = z * kShrinkK + 512 * q + 8 * lane;
+        u32 w[2] = {0u, 0u};
+        if (e0 + 8 <= p.k) {
+            __builtin_memcpy(w, a + e0, 8);
+        } else {
+            for (int e = 0; e < 8 && e0 + e < p.k; ++e) {
+                const u32 b = (u32)(uint8_t)a[e0 + e] << (8 * (e & 3));
+                if (e < 4) w[0] |= b;
+                else w[1] |= b;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[q][e] = (float)(int8_t)(w[e >> 2] >> (8 * (e & 3)));
+    }
+    float f = p.scale_a != nullptr ? p.scale_a[i] : 1.0f;
+    if (ad.scaling != nullptr) f *= ad.scaling[which];
+    const uint16_t *down = (const uint16_t *)ad.down + which * ad.stride_down;
+    const bool bf = ad.type == IGEMM_BF16;
+    // Four ranks at a time, so that their loads are in flight together.
+    for (int r0 = 4 * wave; r0 < rank; r0 += 4 * WAVES) {
+        u32 w[4][PASS][4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int q = 0; q < PASS; ++q) {
+                const int e0 = min(z * kShrinkK + 512 * q + 8 * lane, p.k);
+                load8(down + min(r0 + b, rank - 1) * ad.ld_down, e0, p.k, p.k, w[b][q]);
+            }
+        float s[4] = {};
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int q = 0; q < PASS; ++q)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint16_t v = (uint16_t)(w[b][q][e / 2] >> (16 * (e & 1)));
+                    s[b] = fmaf(x[q][e], bf ? from16<IGEMM_BF16>(v) : from16<IGEMM_F16>(v), s[b]);
+                }
+#pragma unroll
+        for (int o = 32; o > 0; o /= 2)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) s[b] += __shfl_xor(s[b], o);
+        if (lane == 0)
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                if (r0 + b < rank) u[((int64_t)z * p.rows + i) * rpad + r0 + b] = s[b] * f;
+    }
+}
+
 // BM x BN: the workgroup's tile, WM x WN a wave's; NST ring stages; OCC
 // workgroups a compute unit; REG: through registers; PART: the raw sums of k
 // slice z go to part[z][position][column] instead; ADAPT: adapters beside, with
 // u in ks parts of rows x rpad floats.
+//
+// A sliced product's adapters (PART and ADAPT): the first rows x ks workgroups
+// compute u (shrink_row) beside the product's.
 template <int BM, int BN, int WM, int WN, int NST, int OCC, bool REG, bool PART, bool ADAPT>
 __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, OCC *((BM / WM) * (BN / WN)) / 4)
-rows_tile(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
+rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int rpad,
           int32_t *__restrict__ part, int slices, int kchunk) {
     typedef Mfma<32> M;
     constexpr int TM = WM / 32, TN = WN / 32;
@@ -96,18 +167,29 @@ rows_tile(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
     constexpr int DPA = APL / 1024 / NW, DPB = BPL / 1024 / NW, DPW = DPA + DPB;
     static_assert(NST >= 2 && (NST - 2) * DPW < 64, "outstanding DMA count");
     static_assert(!REG || NST == 2, "two stages through registers");
-    static_assert(OCC * (NST * STAGE + 16 * BM) <= 160 * 1024, "LDS");
-    // A wave's output block of 32 rows, in pieces of 16 bytes.
-    constexpr int PITCH = WN * 4 + 16;
-    static_assert(NW * 32 * PITCH <= NST * STAGE, "output blocks fit the ring");
+    // A wave's output block: 32 rows x JB blocks of 32 columns at a time (the
+    // registers beside the sums), in pieces of 16 bytes.
+    constexpr int JB = TN < 2 ? TN : 2, PITCH = 32 * JB * 4 + 16;
+    constexpr int SMEM = NST * STAGE > NW * 32 * PITCH ? NST * STAGE : NW * 32 * PITCH;
+    static_assert(TN % JB == 0, "whole output blocks");
+    static_assert(OCC * (SMEM + 16 * BM) <= 160 * 1024, "LDS");
 
-    __shared__ __attribute__((aligned(1024))) char smem[NST * STAGE];
+    __shared__ __attribute__((aligned(1024))) char smem[SMEM];
     __shared__ __attribute__((aligned(16))) int arow[BM], orow[BM], arow_id[BM];
     __shared__ __attribute__((aligned(16))) float arow_s[BM];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm0 = (wave / WGN) * WM, wn0 = (wave % WGN) * WN;
+
+    int first = 0;
+    if constexpr (PART && ADAPT) {
+        first = p.rows * ks;
+        if ((int)blockIdx.x < first) {
+            shrink_row<NW>(p, ad, u, rpad, (int)blockIdx.x % p.rows, (int)blockIdx.x / p.rows);
+            return;
+        }
+    }
 
     // ---- which tile -----------------------------------------------------------
     const int tiles_n = (p.n + BN - 1) / BN;
@@ -120,7 +202,8 @@ rows_tile(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
     int64_t at;
     {
         const int64_t q = total >> 3;
-        const int r = (int)(total & 7), x = blockIdx.x & 7, i = blockIdx.x >> 3;
+        const int b = (int)blockIdx.x - first;
+        const int r = (int)(total & 7), x = b & 7, i = b >> 3;
         if (i >= q + (x < r)) return;
         at = x * q + min(x, r) + i;
     }
@@ -146,7 +229,7 @@ rows_tile(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
         arow[r] = a;
         orow[r] = o;
         if constexpr (!PART) arow_s[r] = a >= 0 && p.scale_a != nullptr ? p.scale_a[a] : 1.0f;
-        if constexpr (ADAPT) {
+        if constexpr (ADAPT && !PART) {
             const int w = a >= 0 ? ad.ids[a] : -1;
             arow_id[r] = w >= 0 && w < ad.adapters ? w : -1;
         }
@@ -207,10 +290,25 @@ rows_tile(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
     auto load = [&](regs_a &va, regs_b &vb, int kt) __attribute__((always_inline)) {
         if constexpr (REG) {
             const int k0 = kt * BK, left = klen - k0;
+            const char *bk = b_base + (int64_t)k0 * ldb;
+            // A k-tile inside both matrices takes plain loads, all in flight at
+            // once. (What A's rows have past the k range meets zeros of B.)
+            const bool inside = k0 + BK <= klen &&
+                                (int64_t)(kbeg + k0 + BK - 1) * ldb + n0 + BN <=
+                                    (int64_t)(p.k - 1) * ldb + p.n;
+            if (inside) {
+#pragma unroll
+                for (int d = 0; d < DPA; ++d)
+                    va[d] = ring::load_u16(a_base + (u32)(max(arow[a_row[d]], 0) * lda + k0 +
+                                                          16 * a_lc[d]));
+#pragma unroll
+                for (int d = 0; d < DPB; ++d)
+                    vb[d] = ring::load_u16(bk + (u32)(b_row[d] * ldb + 16 * b_lc[d]));
+                return;
+            }
             const int a_end = (int)((int64_t)(p.a_rows - 1) * lda + p.k - kbeg);
             const bool a_tiny = (int64_t)(p.a_rows - 1) * lda + p.k < 16;
             const bool b_tiny = (int64_t)(p.k - 1) * ldb + p.n < 16;
-            const char *bk = b_base + (int64_t)k0 * ldb;
             const int b_end =
                 (int)min((int64_t)(p.k - 1 - kbeg - k0) * ldb + p.n - n0, (int64_t)0x7fffffff);
 #pragma unroll
@@ -260,7 +358,11 @@ rows_tile(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+    // A wave whose rows or columns all lie outside leaves the matrix cores to the
+    // others (the last row tile of a group is part empty).
+    const bool busy = wm0 < mrows && n0 + wn0 < p.n;
     auto tile = [&](int s) __attribute__((always_inline)) {
+        if (!busy) return;
         const char *st = smem + s * STAGE;
 #pragma unroll
         for (int q = 0; q < KS; ++q) {
@@ -328,6 +430,7 @@ rows_tile(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
     // ---- scales, adapters, output -------------------------------------------------------
     __syncthreads();  // the ring becomes the waves' output blocks
     char *blk = smem + wave * 32 * PITCH;
+    if (!busy) return;
     float sb[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
@@ -336,11 +439,12 @@ rows_tile(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
     }
     auto emit = [&](auto type_c) __attribute__((always_inline)) {
         constexpr int T = decltype(type_c)::value;
-        constexpr int ES = T == IGEMM_F32 ? 4 : 2, V = 16 / ES, LPR = WN / V;  // lanes a row
+        constexpr int ES = T == IGEMM_F32 ? 4 : 2, V = 16 / ES, LPR = 32 * JB / V;  // lanes a row
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int r0 = wm0 + 32 * i;
-            float x[TN][16];
+        for (int ij = 0; ij < TM * (TN / JB); ++ij) {
+            const int i = ij / (TN / JB), jb = ij % (TN / JB) * JB;
+            const int r0 = wm0 + 32 * i, c0 = n0 + wn0 + 32 * jb;
+            float x[JB][16];
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const float4 s = *(const float4 *)(arow_s + r0 + M::out_row(lane, r));
@@ -348,8 +452,8 @@ rows_tile(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
 #pragma unroll
-                    for (int j = 0; j < TN; ++j)
-                        x[j][r + q] = (float)acc[i][j][r + q] * sa[q] * sb[j];
+                    for (int j = 0; j < JB; ++j)
+                        x[j][r + q] = (float)acc[i][jb + j][r + q] * sa[q] * sb[jb + j];
             }
             if constexpr (ADAPT) {
                 // The block's adapters, one after the other: every row is
@@ -364,9 +468,9 @@ rows_tile(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
                         __builtin_amdgcn_readlane(mine, __ffsll((unsigned long long)todo) - 1);
                     todo &= ~__ballot(mine == which);
                     const int rank = rank_of(ad, which);
-                    v16f y[TN];
+                    v16f y[JB];
 #pragma unroll
-                    for (int j = 0; j < TN; ++j)
+                    for (int j = 0; j < JB; ++j)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) y[j][r] = 0.0f;
                     for (int e0 = 0; e0 < rank; e0 += 16) {
@@ -390,8 +494,8 @@ rows_tile(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
                         v8bf u1, u2, u3;
                         split3(uv, u1, u2, u3);
 #pragma unroll
-                        for (int j = 0; j < TN; ++j) {
-                            const int c = min(n0 + wn0 + 32 * j + fr, p.n - 1);
+                        for (int j = 0; j < JB; ++j) {
+                            const int c = min(c0 + 32 * j + fr, p.n - 1);
                             u32 w[4];
                             load8((const uint16_t *)ad.up + which * ad.stride_up + c * ad.ld_up,
                                   e, ad.rank, rank, w);
@@ -424,22 +528,22 @@ rows_tile(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
 #pragma unroll
                         for (int q = 0; q < 4; ++q)
 #pragma unroll
-                            for (int j = 0; j < TN; ++j)
+                            for (int j = 0; j < JB; ++j)
                                 x[j][r + q] = ids[q] == which ? x[j][r + q] + y[j][r + q]
                                                               : x[j][r + q];
                     }
                 }
             }
-            constexpr int P = WN * ES + 16;  // (the pad keeps four rows off one bank)
+            constexpr int P = 32 * JB * ES + 16;  // (the pad keeps four rows off one bank)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
+                for (int j = 0; j < JB; ++j)
                     put<T>(blk + M::out_row(lane, r) * P, 32 * j + M::out_col(lane), x[j][r]);
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            const int c = (lane % LPR) * V, col = n0 + wn0 + c;
+            const int c = (lane % LPR) * V, col = c0 + c;
 #pragma unroll
             for (int q = 0; q < 32; q += 64 / LPR) {
                 const int lr = q + lane / LPR;
