@@ -10,7 +10,9 @@ namespace igemm {
 namespace rows {
 namespace {
 
-typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef v8hf v8h;
+typedef short v8s __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ int byte_of(u32 w, int b) { return (int)(int8_t)(w >> (8 * b)); }
 
@@ -23,100 +25,151 @@ __device__ __forceinline__ v4i load_row16(const int8_t *row, int e0, int len) {
 // ---- u = scaling scale_a A down^T -------------------------------------------------
 
 // Few rows or few ranks, where the product is not sliced (shrink_row).
+template <int T>
 __global__ void __launch_bounds__(256)
 shrink_rows(Product p, Adapters ad, float *__restrict__ u, int rpad) {
-    shrink_row<4>(p, ad, u, rpad, blockIdx.x, blockIdx.y);
+    shrink_row<4, T>(p, ad, u, rpad, p.k, blockIdx.x, 0);
 }
 
-// Many rows: 32 rows x 32 ranks a workgroup on the matrix cores, k over its eight
-// waves, whose sums meet in LDS. int8 values are exact in both 16-bit types.
-// The block's adapters are taken one after the other, as in the tile kernel.
-template <int T>
+// Many rows: 32 rows x 16 NR ranks a workgroup, on the matrix cores (int8 values are
+// exact in both 16-bit types): two waves of 16 rows for each of four k groups of
+// 128 k at a time, whose sums meet in LDS at the end. Both operands pass through LDS,
+// read along their rows: fragments read straight from memory take 32 rows a load,
+// which at a row stride of a power of two all lie in one channel of the cache
+// (8192 x 4096, rank 16, 24 adapters: 31 us, against 24 here). The block's adapters are shared
+// out to gridDim.z workgroups, each of which takes its own one after the other:
+// where one request ends and the next begins, a block has two.
+constexpr int kShrinkRows = 32, kShrinkTile = 512, kShrinkTurns = 3;
+template <int T, int NR>
 __global__ void __launch_bounds__(512)
 shrink_tiles(Product p, Adapters ad, float *__restrict__ u, int rpad) {
-    __shared__ float red[8][32][33];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int i0 = blockIdx.x * 32, r0 = blockIdx.y * 32;
-    const int row = min(i0 + (lane & 31), p.rows - 1), half = lane >> 5;
-    int mine = i0 + (lane & 31) < p.rows ? ad.ids[row] : -1;
+    constexpr int DR = 16 * NR;  // ranks
+    __shared__ __attribute__((aligned(16))) char sa[2][4][kShrinkRows * 128];
+    __shared__ __attribute__((aligned(16))) char sd[2][4][DR * 256];
+    __shared__ __attribute__((aligned(16))) v4f red[3][2][NR][64];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int i0 = blockIdx.x * kShrinkRows, r0 = blockIdx.y * DR;
+    const int nkt = (p.k + kShrinkTile - 1) / kShrinkTile;
+    const int at = i0 + (lane & 31);
+    int mine = at < p.rows ? ad.ids[at] : -1;
     if (mine >= ad.adapters) mine = -1;
-    const int8_t *a = p.A + (int64_t)row * p.lda;
-    const int span = ((p.k + 7) / 8 + 31) / 32 * 32;  // k of a wave
-    const int kb = wave * span, ke = min(kb + span, p.k);
     uint64_t todo = __ballot(mine >= 0);
+    const int q = lane >> 4, c = lane & 15;
+    const int kg = wave >> 1, rw = wave & 1;  // k group, row block
+    int turn = 0;
     while (todo != 0) {
         const int which =
             __builtin_amdgcn_readlane(mine, __ffsll((unsigned long long)todo) - 1);
         todo &= ~__ballot(mine == which);
+        if (turn++ % (int)gridDim.z != (int)blockIdx.z) continue;
         const int rank = rank_of(ad, which);
-        if (r0 >= rank) continue;
-        const int r = min(r0 + (lane & 31), rank - 1);
-        const uint16_t *d =
-            (const uint16_t *)ad.down + which * ad.stride_down + r * ad.ld_down;
-        v16f acc;
+        const uint16_t *down = (const uint16_t *)ad.down + which * ad.stride_down;
+        // Sixteen lanes a row of A, thirty-two a row of `down`. Rows past the end and
+        // ranks past the adapter's read the last one: nothing comes of them.
+        v4i av[2][2], dv[2][2 * NR];  // two k-tiles on their way
+        auto load = [&](auto set, int kt) __attribute__((always_inline)) {
+            constexpr int S = decltype(set)::value;
+            const int k0 = kt * kShrinkTile;
+            const int8_t *arow = p.A + (int64_t)min(i0 + (tid >> 4), p.rows - 1) * p.lda;
 #pragma unroll
-        for (int q = 0; q < 16; ++q) acc[q] = 0.0f;
-        // 32 k in two instructions: lane half h holds k 16 h .. 16 h + 15 of both
-        // operands, eight at a time.
-        auto step = [&](v4i av, const v4i (&dv)[2]) __attribute__((always_inline)) {
+            for (int x = 0; x < 2; ++x)
+                av[S][x] = load_row16(arow, k0 + 256 * x + 16 * (tid & 15), p.k);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                if constexpr (T == IGEMM_BF16) {
-                    v8bf x;
+            for (int n = 0; n < NR; ++n) {
+                const int r = max(min(r0 + 16 * n + (tid >> 5), rank - 1), 0);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        x[e] = (__bf16)(float)byte_of((u32)av[2 * q + e / 4], e & 3);
-                    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        x, __builtin_bit_cast(v8bf, dv[q]), acc, 0, 0, 0);
-                } else {
-                    v8h x;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        x[e] = (_Float16)(float)byte_of((u32)av[2 * q + e / 4], e & 3);
-                    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                        x, __builtin_bit_cast(v8h, dv[q]), acc, 0, 0, 0);
+                for (int x = 0; x < 2; ++x) {
+                    u32 w[4];
+                    load8(down + r * ad.ld_down, min(k0 + 256 * x + 8 * (tid & 31), p.k), p.k, p.k,
+                          w);
+                    dv[S][2 * n + x] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
                 }
             }
         };
-        // Four steps' loads before the first is used; the last k apart, bounded.
-        int k0 = kb;
-        constexpr int AHEAD = 4;
-        for (; k0 + 32 * AHEAD <= ke; k0 += 32 * AHEAD) {
-            v4i av[AHEAD], dv[AHEAD][2];
+        auto store = [&](auto set) __attribute__((always_inline)) {
+            constexpr int s = decltype(set)::value;
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x) {
-                const int e0 = k0 + 32 * x + 16 * half;
-                av[x] = ring::load_u16((const char *)a + e0);
-                dv[x][0] = ring::load_u16((const char *)(d + e0));
-                dv[x][1] = ring::load_u16((const char *)(d + e0 + 8));
+            for (int x = 0; x < 2; ++x) {
+                const int row = tid >> 4, ch = 16 * x + (tid & 15);
+                *(v4i *)(sa[s][ch >> 3] + row * 128 + 16 * ((ch & 7) ^ (row & 7))) = av[s][x];
             }
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x) step(av[x], dv[x]);
-        }
-        for (; k0 < ke; k0 += 32) {
-            const int e0 = k0 + 16 * half;
-            v4i dv[2];
+            for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                u32 w[4];
-                load8(d, e0 + 8 * q, p.k, p.k, w);
-                dv[q] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+                for (int x = 0; x < 2; ++x) {
+                    const int row = 16 * n + (tid >> 5), ch = 32 * x + (tid & 31);
+                    *(v4i *)(sd[s][ch >> 4] + row * 256 + 16 * ((ch & 15) ^ (row & 15))) =
+                        dv[s][2 * n + x];
+                }
+        };
+        v4f acc[NR];
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[n][e] = 0.0f;
+        if (rank > r0) {
+            load(ic<0>{}, 0);
+            if (nkt > 1) load(ic<1>{}, 1);
+            store(ic<0>{});
+            auto step = [&](auto set, int kt) __attribute__((always_inline)) {
+                constexpr int s = decltype(set)::value;
+                __syncthreads();
+                if (kt + 2 < nkt) load(ic<s>{}, kt + 2);
+                // 32 k an instruction: lane group q holds k 8 q .. 8 q + 7 of both.
+                const int row = 16 * rw + c;
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) {
+                    const int chunk = 2 * ks + (q >> 1);
+                    const u32 *src = (const u32 *)(sa[s][kg] + row * 128 +
+                                                   16 * (chunk ^ (row & 7)) + 8 * (q & 1));
+                    const u32 w[2] = {src[0], src[1]};
+                    v8s x;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        x[e] = (short)to16<T>((float)byte_of(w[e >> 2], e & 3));
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) {
+                        const v4i d = *(const v4i *)(sd[s][kg] + (16 * n + c) * 256 +
+                                                     16 * ((4 * ks + q) ^ c));
+                        if constexpr (T == IGEMM_BF16)
+                            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                __builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, d), acc[n], 0,
+                                0, 0);
+                        else
+                            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                                __builtin_bit_cast(v8h, x), __builtin_bit_cast(v8h, d), acc[n], 0,
+                                0, 0);
+                    }
+                }
+                if (kt + 1 < nkt) store(ic<1 - s>{});
+            };
+            for (int kt = 0; kt < nkt; kt += 2) {
+                step(ic<0>{}, kt);
+                if (kt + 1 < nkt) step(ic<1>{}, kt + 1);
             }
-            step(load_row16(a, e0, p.k), dv);
         }
         __syncthreads();
+        if (kg > 0)
 #pragma unroll
-        for (int q = 0; q < 16; ++q)
-            red[wave][Mfma<32>::out_row(lane, q)][lane & 31] = acc[q];
+            for (int n = 0; n < NR; ++n) red[kg - 1][rw][n][lane] = acc[n];
         __syncthreads();
+        if (kg > 0) continue;
         const float f = ad.scaling != nullptr ? ad.scaling[which] : 1.0f;
-        for (int e = threadIdx.x; e < 1024; e += 512) {
-            const int lr = e >> 5, c = e & 31, i = i0 + lr;
-            if (i < p.rows && r0 + c < rank && ad.ids[i] == which) {
-                float s = 0.0f;
 #pragma unroll
-                for (int w = 0; w < 8; ++w) s += red[w][lr][c];
-                u[(int64_t)i * rpad + r0 + c] = s * (p.scale_a != nullptr ? p.scale_a[i] : 1.0f) * f;
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int g = 0; g < 3; ++g) acc[n] += red[g][rw][n][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int lr = 16 * rw + 4 * q + e, i = i0 + lr;
+            if (__shfl(mine, lr) != which) continue;
+            const float sc = p.scale_a != nullptr ? p.scale_a[i] : 1.0f;
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+                const int r = r0 + 16 * n + c;
+                if (r < rpad)
+                    u[(int64_t)i * rpad + r] = r < rank ? acc[n][e] * sc * f : 0.0f;
             }
         }
     }
@@ -258,11 +311,13 @@ combine_slots(int64_t tokens, int top_k, int n, const char *Z, int64_t ldz,
 
 // ---- choices --------------------------------------------------------------------------
 
+constexpr int kShrinkK = 1024;  // k a workgroup of a sliced product's shrink_row
+
 struct Choice {
     int bm, bn;       // tile
     int slices, kchunk;
-    bool by_row;      // u: a workgroup a row (ks k slices), else 32 x 32 blocks
-    int ks, rpad;
+    bool by_row;      // u: a workgroup a row (and k slice, where the product is
+    int ks, rpad;     // sliced: ks of kShrinkK), else blocks of 32 rows
     int64_t u_bytes, part_bytes;
 };
 
@@ -282,8 +337,8 @@ Choice choose(int64_t rows, int64_t n, int64_t k, int64_t groups, int64_t adapte
     if (avg <= 32) {
         c.bm = 32, c.bn = 256;
     } else if (avg <= 64 || tiles(128, 128) < num_cu) {
-        c.bm = 64, c.bn = 256;
-    } else if (avg >= 192 &&
+        c.bm = 64, c.bn = 128;
+    } else if (avg >= 192 && adapters == 0 &&
                full(tiles(256, 256), num_cu) >= 0.9 * full(tiles(128, 128), 2 * num_cu)) {
         c.bm = 256, c.bn = 256;
     } else {
@@ -291,7 +346,7 @@ Choice choose(int64_t rows, int64_t n, int64_t k, int64_t groups, int64_t adapte
     }
     // Fewer tiles than compute units: narrower ones, then k slices.
     int64_t slices = 1;
-    if (c.bm <= 64 && tiles(c.bm, 256) < num_cu) {
+    if (c.bm <= 64 && tiles(c.bm, c.bn) < num_cu) {
         c.bn = 128;
         const int64_t t = tiles(c.bm, 128);
         if (2 * t <= num_cu) slices = num_cu / t;
@@ -305,9 +360,9 @@ Choice choose(int64_t rows, int64_t n, int64_t k, int64_t groups, int64_t adapte
     c.slices = k > 0 ? (int)ceil_div(k, chunk) : 1;
     if (c.slices > 1) c.part_bytes = up256(c.slices * rows * n * 4);
     if (adapters > 0 && rank > 0) {
-        c.rpad = (int)(ceil_div(rank, 16) * 16);
+        c.rpad = (int)(ceil_div(rank, 32) * 32);  // (a row's 32 ranks: one line)
         c.by_row = c.slices > 1 || rows * rank <= 4096;
-        c.ks = c.by_row ? (int)ceil_div(k, kShrinkK) : 1;
+        c.ks = c.slices > 1 ? (int)ceil_div(k, kShrinkK) : 1;
         c.u_bytes = up256(c.ks * rows * c.rpad * 4);
     }
     return c;
@@ -319,24 +374,30 @@ int64_t most_tiles(int64_t rows, int64_t groups, int64_t bm) {
     return (rows + used * (bm - 1)) / bm;
 }
 
+template <int BM, int BN, int WM, int WN, int NST, int OCC, bool REG, int ADAPT>
+const void *pick_part(bool part) {
+    if (!part) return (const void *)rows_tile<BM, BN, WM, WN, NST, OCC, REG, false, ADAPT>;
+    if constexpr (BM <= 64 && BN == 128)
+        return (const void *)rows_tile<BM, BN, WM, WN, NST, OCC, REG, true, ADAPT>;
+    return nullptr;
+}
+// adapt: the adapters' weight type, 0 for none.
 template <int BM, int BN, int WM, int WN, int NST, int OCC, bool REG>
-const void *pick_epi(bool part, bool adapt) {
-    if (part) {
-        if constexpr (BM <= 64 && BN == 128)
-            return adapt ? (const void *)rows_tile<BM, BN, WM, WN, NST, OCC, REG, true, true>
-                         : (const void *)rows_tile<BM, BN, WM, WN, NST, OCC, REG, true, false>;
-        return nullptr;
-    }
-    return adapt ? (const void *)rows_tile<BM, BN, WM, WN, NST, OCC, REG, false, true>
-                 : (const void *)rows_tile<BM, BN, WM, WN, NST, OCC, REG, false, false>;
+const void *pick_epi(bool part, int adapt) {
+    if constexpr (BM == 256)  // (with adapters its registers spill)
+        return adapt == 0 ? pick_part<BM, BN, WM, WN, NST, OCC, REG, 0>(part) : nullptr;
+    return adapt == 0            ? pick_part<BM, BN, WM, WN, NST, OCC, REG, 0>(part)
+           : adapt == IGEMM_BF16 ? pick_part<BM, BN, WM, WN, NST, OCC, REG, IGEMM_BF16>(part)
+                                 : pick_part<BM, BN, WM, WN, NST, OCC, REG, IGEMM_F16>(part);
 }
 // The tile's kernel and its threads. (us, random operands that are not cached:
 // 64 rows of 64 experts, 1024 x 2048: 32 x 256 20.5, 32 x 128 23.5; 4096 rows,
-// 2048 x 1024: 64 x 256 41.9, 64 x 128 42.4, 128 x 128 47.9; 32768 rows, 4096 x 2048:
-// 256 x 256 358, 128 x 256 404, 128 x 128 442; one weight, 8192 x 11008 x 4096: 351,
-// 377, 391; 2048 x 4096 x 4096, 128 tiles of 256 x 256: 53, else 38.)
-const void *pick(int bm, int bn, bool reg, bool part, bool adapt, int *threads) {
-    *threads = bm == 256 || (bm == 64 && bn == 256 && !reg) ? 512 : 256;
+// 2048 x 1024: 64 x 128 43.5, 64 x 256 47.7, 128 x 128 47.9; 32768 rows, 4096 x 2048:
+// 256 x 256 366, 128 x 256 400, 128 x 128 430; one weight, 8192 x 11008 x 4096: 367,
+// 397, 388, with adapters of rank 16 430, 458, 432; 2048 x 4096 x 4096, 128 tiles of
+// 256 x 256: 57, else 40.)
+const void *pick(int bm, int bn, bool reg, bool part, int adapt, int *threads) {
+    *threads = bm == 256 ? 512 : 256;
     if (reg)
         return bm == 32    ? (bn == 256 ? pick_epi<32, 256, 32, 64, 2, 2, true>(part, adapt)
                                         : pick_epi<32, 128, 32, 32, 2, 2, true>(part, adapt))
@@ -344,10 +405,9 @@ const void *pick(int bm, int bn, bool reg, bool part, bool adapt, int *threads) 
                            : pick_epi<128, 128, 64, 64, 2, 2, true>(part, adapt);
     return bm == 32    ? (bn == 256 ? pick_epi<32, 256, 32, 64, 4, 1, false>(part, adapt)
                                     : pick_epi<32, 128, 32, 32, 3, 2, false>(part, adapt))
-           : bm == 64  ? (bn == 256 ? pick_epi<64, 256, 32, 64, 3, 1, false>(part, adapt)
-                                    : pick_epi<64, 128, 32, 64, 3, 2, false>(part, adapt))
+           : bm == 64  ? pick_epi<64, 128, 32, 64, 3, 2, false>(part, adapt)
            : bm == 128 ? pick_epi<128, 128, 64, 64, 2, 2, false>(part, adapt)
-                       : pick_epi<256, 256, 128, 64, 2, 1, false>(part, adapt);
+                       : pick_epi<256, 256, 64, 128, 2, 1, false>(part, adapt);
 }
 
 }  // namespace
@@ -370,31 +430,46 @@ int launch_product(const Product &p, const Adapters &ad, int num_cu, void *works
     // registers for it.
     const bool reg = (uintptr_t)p.A % 4 != 0 || (uintptr_t)p.B % 4 != 0 || p.lda % 4 != 0 ||
                      p.ldb % 4 != 0 || p.stride_b % 4 != 0 ||
-                     ((int64_t)p.k + kStepK) * p.ldb > 0xffffffffll;
+                     ((int64_t)p.k + kStepK) * p.ldb > 0xffffffffll ||
+                     (ad.adapters > 0 && c.slices == 1 &&
+                      ((uintptr_t)ad.up % 4 != 0 || ad.ld_up % 2 != 0 || ad.stride_up % 2 != 0 ||
+                       (int64_t)p.rows * c.rpad * 4 > 0x7fffffff));
     int bm = c.bm, bn = c.bn, threads = 0;
     if (reg && bm >= 64) bn = 128;
     if (reg && bm == 256) bm = 128;
-    const void *fn = pick(bm, bn, reg, sliced, adapt, &threads);
+    const void *fn = pick(bm, bn, reg, sliced, adapt ? ad.type : 0, &threads);
     const int64_t first = sliced && adapt ? (int64_t)p.rows * c.ks : 0;
     const int64_t grid = first + most_tiles(p.rows, p.groups, bm) * ceil_div(p.n, bn) * c.slices;
     if (fn == nullptr || grid > 0x7fffffff) return IGEMM_ENOTSUP;
     if (adapt && !sliced) {
         if (c.by_row) {
-            const dim3 g((unsigned)p.rows, (unsigned)c.ks);
-            shrink_rows<<<g, 256, 0, stream>>>(p, ad, u, c.rpad);
-        } else {
-            const dim3 g((unsigned)((p.rows + 31) / 32), (unsigned)((ad.rank + 31) / 32));
             if (ad.type == IGEMM_BF16)
-                shrink_tiles<IGEMM_BF16><<<g, 512, 0, stream>>>(p, ad, u, c.rpad);
+                shrink_rows<IGEMM_BF16><<<dim3((unsigned)p.rows), 256, 0, stream>>>(p, ad, u, c.rpad);
             else
-                shrink_tiles<IGEMM_F16><<<g, 512, 0, stream>>>(p, ad, u, c.rpad);
+                shrink_rows<IGEMM_F16><<<dim3((unsigned)p.rows), 256, 0, stream>>>(p, ad, u, c.rpad);
+        } else {
+            // 32 ranks a workgroup, or 16 where that fills the compute units better.
+            const int64_t blocks = ceil_div(p.rows, kShrinkRows);
+            const bool two = ad.rank > 16 && blocks * ceil_div(ad.rank, 32) >= num_cu;
+            const dim3 g((unsigned)blocks, (unsigned)ceil_div(ad.rank, two ? 32 : 16), kShrinkTurns);
+            const bool bf = ad.type == IGEMM_BF16;
+            const void *sh = two ? bf ? (const void *)shrink_tiles<IGEMM_BF16, 2>
+                                      : (const void *)shrink_tiles<IGEMM_F16, 2>
+                             : bf ? (const void *)shrink_tiles<IGEMM_BF16, 1>
+                                  : (const void *)shrink_tiles<IGEMM_F16, 1>;
+            Product sp = p;
+            Adapters sad = ad;
+            int rpad = c.rpad;
+            void *args[] = {&sp, &sad, &u, &rpad};
+            if (hipLaunchKernel(sh, g, dim3(512), args, 0, stream) != hipSuccess)
+                return IGEMM_EHIP;
         }
         if (hipGetLastError() != hipSuccess) return IGEMM_EHIP;
     }
     Product pp = p;
     Adapters aa = ad;
-    int ks = c.ks, rpad = c.rpad, slices = c.slices, kchunk = c.kchunk;
-    void *args[] = {&pp, &aa, &u, &ks, &rpad, &part, &slices, &kchunk};
+    int ks = c.ks, kshrink = kShrinkK, rpad = c.rpad, slices = c.slices, kchunk = c.kchunk;
+    void *args[] = {&pp, &aa, &u, &ks, &kshrink, &rpad, &part, &slices, &kchunk};
     if (hipLaunchKernel(fn, dim3((unsigned)grid), dim3((unsigned)threads), args, 0, stream) !=
         hipSuccess)
         return IGEMM_EHIP;

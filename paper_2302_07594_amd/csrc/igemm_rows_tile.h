@@ -31,9 +31,13 @@ using ring::v4u;
 
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef _Float16 v8hf __attribute__((ext_vector_type(8)));
 
 // The ring of k-tiles: 128 k, one whole line of a row of A.
 constexpr int kStepK = 128;
+
+__device__ __forceinline__ int as_int(float x) { return __builtin_bit_cast(int, x); }
+__device__ __forceinline__ float as_float(int x) { return __builtin_bit_cast(float, x); }
 
 // 8 values as bf16 parts hi + mid + lo, each the rounding of what the ones
 // before it leave: 24 bits together. An infinite or NaN value is its hi alone.
@@ -78,63 +82,58 @@ __device__ __forceinline__ int rank_of(const Adapters &ad, int which) {
     return ad.ranks != nullptr ? min(max(ad.ranks[which], 0), ad.rank) : ad.rank;
 }
 
-// u = scaling scale_a A down^T for few rows or few ranks: row i and k slice z by
-// one workgroup, every wave a rank in WAVES at a time, 16 bytes of `down` a lane.
-// What it reads of `down` is one adapter a row, whichever the row's is, so a
-// batch of 16 requests with an adapter each takes as long as one with a shared
-// one.
-constexpr int kShrinkK = 1024;  // k a workgroup: two passes of 64 lanes x 8
-template <int WAVES>
+// u = scaling scale_a A down^T for few rows or few ranks: row i and k slice z (of
+// kslice) by one workgroup, every wave four ranks at a time, 16 bytes of `down` a
+// lane. What it reads of `down` is one adapter a row, whichever the row's is, so
+// a batch of 16 requests with an adapter each takes as long as one with a shared
+// one. Ranks up to rpad that the adapter does not have are zeros.
+template <int WAVES, int T>
 __device__ void shrink_row(const Product &p, const Adapters &ad, float *__restrict__ u, int rpad,
-                           int i, int z) {
+                           int kslice, int i, int z) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int which = ad.ids[i];
     const int rank = rank_of(ad, which);
     if (rank == 0) return;
     const int8_t *a = p.A + (int64_t)i * p.lda;
-    constexpr int PASS = kShrinkK / 512;
-    float x[PASS][8];
-#pragma unroll
-    for (int q = 0; q < PASS; ++q) {
-        const int e0 = z * kShrinkK + 512 * q + 8 * lane;
-        u32 w[2] = {0u, 0u};
-        if (e0 + 8 <= p.k) {
-            __builtin_memcpy(w, a + e0, 8);
-        } else {
-            for (int e = 0; e < 8 && e0 + e < p.k; ++e) {
-                const u32 b = (u32)(uint8_t)a[e0 + e] << (8 * (e & 3));
-                if (e < 4) w[0] |= b;
-                else w[1] |= b;
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[q][e] = (float)(int8_t)(w[e >> 2] >> (8 * (e & 3)));
-    }
     float f = p.scale_a != nullptr ? p.scale_a[i] : 1.0f;
     if (ad.scaling != nullptr) f *= ad.scaling[which];
     const uint16_t *down = (const uint16_t *)ad.down + which * ad.stride_down;
-    const bool bf = ad.type == IGEMM_BF16;
-    // Four ranks at a time, so that their loads are in flight together.
+    const int kb = z * kslice, ke = min(p.k, kb + kslice);
+    constexpr int PASS = 2;  // of 64 lanes x 8 k, all their loads in flight together
     for (int r0 = 4 * wave; r0 < rank; r0 += 4 * WAVES) {
-        u32 w[4][PASS][4];
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
+        float s[4] = {};
+        for (int k0 = kb; k0 < ke; k0 += 512 * PASS) {
+            u32 x[PASS][2], w[4][PASS][4];
 #pragma unroll
             for (int q = 0; q < PASS; ++q) {
-                const int e0 = min(z * kShrinkK + 512 * q + 8 * lane, p.k);
-                load8(down + min(r0 + b, rank - 1) * ad.ld_down, e0, p.k, p.k, w[b][q]);
-            }
-        float s[4] = {};
+                const int e0 = min(k0 + 512 * q + 8 * lane, ke);
+                x[q][0] = x[q][1] = 0u;
+                if (e0 + 8 <= ke) {
+                    __builtin_memcpy(x[q], a + e0, 8);
+                } else {
+                    for (int e = 0; e < 8 && e0 + e < ke; ++e) {
+                        const u32 b = (u32)(uint8_t)a[e0 + e] << (8 * (e & 3));
+                        if (e < 4) x[q][0] |= b;
+                        else x[q][1] |= b;
+                    }
+                }
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+                for (int b = 0; b < 4; ++b)
+                    load8(down + min(r0 + b, rank - 1) * ad.ld_down, e0, p.k, ke, w[b][q]);
+            }
 #pragma unroll
             for (int q = 0; q < PASS; ++q)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const uint16_t v = (uint16_t)(w[b][q][e / 2] >> (16 * (e & 1)));
-                    s[b] = fmaf(x[q][e], bf ? from16<IGEMM_BF16>(v) : from16<IGEMM_F16>(v), s[b]);
+                    const float xe = (float)(int8_t)(x[q][e >> 2] >> (8 * (e & 3)));
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const uint16_t v = (uint16_t)(w[b][q][e / 2] >> (16 * (e & 1)));
+                        s[b] = fmaf(xe, from16<T>(v), s[b]);
+                    }
                 }
+        }
 #pragma unroll
         for (int o = 32; o > 0; o /= 2)
 #pragma unroll
@@ -144,18 +143,20 @@ __device__ void shrink_row(const Product &p, const Adapters &ad, float *__restri
             for (int b = 0; b < 4; ++b)
                 if (r0 + b < rank) u[((int64_t)z * p.rows + i) * rpad + r0 + b] = s[b] * f;
     }
+    for (int r = rank + threadIdx.x; r < rpad; r += WAVES * 64)
+        u[((int64_t)z * p.rows + i) * rpad + r] = 0.0f;
 }
 
 // BM x BN: the workgroup's tile, WM x WN a wave's; NST ring stages; OCC
 // workgroups a compute unit; REG: through registers; PART: the raw sums of k
-// slice z go to part[z][position][column] instead; ADAPT: adapters beside, with
-// u in ks parts of rows x rpad floats.
+// slice z go to part[z][position][column] instead; ADAPT: adapters beside, of this
+// weight type (0: none), u being rows x rpad floats.
 //
 // A sliced product's adapters (PART and ADAPT): the first rows x ks workgroups
-// compute u (shrink_row) beside the product's.
-template <int BM, int BN, int WM, int WN, int NST, int OCC, bool REG, bool PART, bool ADAPT>
+// compute u in ks parts, one a k slice of kshrink (shrink_row), beside the product's.
+template <int BM, int BN, int WM, int WN, int NST, int OCC, bool REG, bool PART, int ADAPT>
 __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, OCC *((BM / WM) * (BN / WN)) / 4)
-rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int rpad,
+rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, int rpad,
           int32_t *__restrict__ part, int slices, int kchunk) {
     typedef Mfma<32> M;
     constexpr int TM = WM / 32, TN = WN / 32;
@@ -172,21 +173,25 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int rpad,
     constexpr int JB = TN < 2 ? TN : 2, PITCH = 32 * JB * 4 + 16;
     constexpr int SMEM = NST * STAGE > NW * 32 * PITCH ? NST * STAGE : NW * 32 * PITCH;
     static_assert(TN % JB == 0, "whole output blocks");
-    static_assert(OCC * (SMEM + 16 * BM) <= 160 * 1024, "LDS");
+    static_assert(OCC * (SMEM + 24 * BM + 16) <= 160 * 1024, "LDS");
 
     __shared__ __attribute__((aligned(1024))) char smem[SMEM];
     __shared__ __attribute__((aligned(16))) int arow[BM], orow[BM], arow_id[BM];
     __shared__ __attribute__((aligned(16))) float arow_s[BM];
+    // The adapters of the tile's rows, each once, and their ranks (by DMA only).
+    constexpr bool XT = ADAPT != 0 && !REG && !PART;
+    __shared__ int uniq[XT ? BM : 1], uniq_rank[XT ? BM : 1], uniq_n;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm0 = (wave / WGN) * WM, wn0 = (wave % WGN) * WN;
 
     int first = 0;
-    if constexpr (PART && ADAPT) {
+    if constexpr (PART && ADAPT != 0) {
         first = p.rows * ks;
         if ((int)blockIdx.x < first) {
-            shrink_row<NW>(p, ad, u, rpad, (int)blockIdx.x % p.rows, (int)blockIdx.x / p.rows);
+            shrink_row<NW, ADAPT>(p, ad, u, rpad, kshrink, (int)blockIdx.x % p.rows,
+                           (int)blockIdx.x / p.rows);
             return;
         }
     }
@@ -228,13 +233,52 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int rpad,
         if (r < mrows) rows_of(p, f.lo + m0 + r, &a, &o);
         arow[r] = a;
         orow[r] = o;
-        if constexpr (!PART) arow_s[r] = a >= 0 && p.scale_a != nullptr ? p.scale_a[a] : 1.0f;
-        if constexpr (ADAPT && !PART) {
+        if constexpr (ADAPT != 0 && !PART) {
             const int w = a >= 0 ? ad.ids[a] : -1;
             arow_id[r] = w >= 0 && w < ad.adapters ? w : -1;
         }
     }
     __syncthreads();
+    // What the output needs of each row and column, fetched behind the first
+    // k-tiles.
+    float sb[TN];
+    auto terms = [&]() __attribute__((always_inline)) {
+        if constexpr (PART) return;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int c = n0 + wn0 + 32 * j + M::out_col(lane);
+            sb[j] = p.scale_b != nullptr && c < p.n ? p.scale_b[(int64_t)f.group * p.n + c] : 1.0f;
+        }
+        for (int r = tid; r < BM; r += NW * 64) {
+            const int a = arow[r];
+            arow_s[r] = a >= 0 && p.scale_a != nullptr ? p.scale_a[a] : 1.0f;
+        }
+        if constexpr (XT) {
+            if (wave == 0) {
+                int n = 0;
+                for (int r0 = 0; r0 < mrows; r0 += 64) {
+                    int id = r0 + lane < BM ? arow_id[min(r0 + lane, BM - 1)] : -1;
+                    for (int q = 0; q < n; ++q) id = id == uniq[q] ? -1 : id;
+                    uint64_t todo = __ballot(id >= 0);
+                    while (todo != 0) {
+                        const int which = __builtin_amdgcn_readlane(
+                            id, __ffsll((unsigned long long)todo) - 1);
+                        todo &= ~__ballot(id == which);
+                        const int rank = rank_of(ad, which);
+                        if (lane == 0 && rank > 0) {
+                            uniq[n] = which;
+                            uniq_rank[n] = rank;
+                        }
+                        n += rank > 0;
+                    }
+                    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                }
+                if (lane == 0) uniq_n = n;
+            }
+        }
+    };
 
     // ---- staging ----------------------------------------------------------------
     int a_row[DPA], a_lc[DPA], b_row[DPB], b_lc[DPB];
@@ -268,6 +312,60 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int rpad,
         Ars = ring::resource(a_base, (u32)(((int64_t)(p.a_rows - 1) * lda + p.k - kbeg + 3) & ~3));
         Brs = ring::resource(b_base, (u32)(((int64_t)(klen - 1) * ldb + p.n - n0 + 3) & ~3));
     }
+    // The adapters' k-tiles follow the product's: two units of 16 ranks of one adapter
+    // each (of different ones, where one ends), u (floats, 64 bytes a row and unit, as
+    // half a row of A) against `up` (32 bytes a column and unit).
+    struct Unit {
+        int q, e0;        // adapter uniq[q], first rank
+        int which, rank;  // that adapter and its rank; which -2: no more units
+    };
+    auto unit_of = [&](int q) __attribute__((always_inline)) -> Unit {
+        Unit x = {q, 0, -2, 0};
+        if constexpr (XT) {
+            if (q < __builtin_amdgcn_readfirstlane(uniq_n)) {
+                x.which = __builtin_amdgcn_readfirstlane(uniq[q]);
+                x.rank = __builtin_amdgcn_readfirstlane(uniq_rank[q]);
+            }
+        }
+        return x;
+    };
+    auto next = [&](Unit x) __attribute__((always_inline)) -> Unit {
+        x.e0 += 16;
+        return x.e0 < x.rank || x.which < 0 ? x : unit_of(x.q + 1);
+    };
+    auto issue_extra = [&](Unit x, int s) __attribute__((always_inline)) {
+        if constexpr (XT) {
+            const Unit y = next(x);
+            const int w0 = x.which, w1 = y.which;
+            const v4u ur = ring::resource((const char *)u,
+                                          w0 >= 0 ? (u32)(p.rows * rpad * 4) : 0u);
+            const u32 up_bytes = (u32)((((int64_t)(p.n - 1) * ad.ld_up + ad.rank) * 2 + 3) & ~3);
+            const u32 base = lds0 + (u32)(s * STAGE);
+#pragma unroll
+            for (int d = 0; d < DPB; ++d) {
+                // 1 KB: 32 columns of two 16-byte chunks, unit after unit
+                const int b = wave * DPB + d;
+                const bool second = b >= BN / 32;
+                const int w = second ? w1 : w0, e0 = second ? y.e0 : x.e0;
+                const int col = (b * 32 + (lane >> 1)) % BN;
+                const int lc = (lane & 1) ^ ((col >> 3) & 1);
+                const v4u br = ring::resource(
+                    (const char *)((const uint16_t *)ad.up + max(w, 0) * ad.stride_up),
+                    w >= 0 && b < BN / 16 ? up_bytes : 0u);
+                ring::dma((u32)min(n0 + col, p.n - 1) * (u32)(ad.ld_up * 2) +
+                              (u32)(e0 * 2 + 16 * lc),
+                          br, base + (u32)(APL + b * 1024));
+            }
+#pragma unroll
+            for (int d = 0; d < DPA; ++d) {
+                const int r = a_row[d], w = a_lc[d] < 4 ? w0 : w1;
+                const int e = (a_lc[d] < 4 ? x.e0 : y.e0) + 4 * (a_lc[d] & 3);
+                ring::dma(arow_id[r] == w ? (u32)max(arow[r], 0) * (u32)(rpad * 4) + 4u * (u32)e
+                                          : 0x80000000u,
+                          ur, base + (u32)((wave * DPA + d) * 1024));
+            }
+        }
+    };
     auto issue = [&](int kt, int s) __attribute__((always_inline)) {
         const bool in = kt < nkt;
         v4u ar = Ars, br = Brs;
@@ -381,17 +479,139 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int rpad,
                 for (int j = 0; j < TN; ++j) acc[i][j] = M::mma(a[i], b[j], acc[i][j]);
         }
     };
+    // The scaled sums take the places of the raw ones.
+    auto scale = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const float4 s = *(const float4 *)(arow_s + wm0 + 32 * i + M::out_row(lane, r));
+                const float sa[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+                        acc[i][j][r + q] = as_int((float)acc[i][j][r + q] * sa[q] * sb[j]);
+            }
+    };
+    auto tile_extra = [&](Unit x, int s) __attribute__((always_inline)) {
+        if constexpr (XT) {
+            if (!busy) return;
+            const char *st = smem + s * STAGE;
+            const int half = lane >> 5;
+#pragma unroll 1
+            for (int h = 0; h < 2 && x.which >= 0; ++h, x = next(x)) {
+                const int which = x.which, left = x.rank - x.e0;
+                // what lies beyond the adapter's rank does not count
+                const int have = left - 8 * half;
+                v8bf v1[TN], v2[TN];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    const int col = wn0 + 32 * j + fr;
+                    v4i b = *(const v4i *)(st + APL + h * (BN * 32) + col * 32 +
+                                           16 * (half ^ ((col >> 3) & 1)));
+                    if (left < 16) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            b[q] = have >= 2 * q + 2 ? b[q] : (have == 2 * q + 1 ? b[q] & 0xffff : 0);
+                    }
+                    v1[j] = __builtin_bit_cast(v8bf, b);
+                    if constexpr (ADAPT == IGEMM_F16) {
+                        // a float16 value is two bf16 parts, exactly
+                        const v8hf hf = __builtin_bit_cast(v8hf, b);
+                        float f8[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) f8[q] = (float)hf[q];
+                        v8bf none;
+                        split3(f8, v1[j], v2[j], none);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    const int row = wm0 + 32 * i + fr;
+                    const uint64_t own = __ballot(arow_id[row] == which);
+                    if (own == 0) continue;
+                    const int ch = 4 * h + 2 * half;
+                    const float4 lo =
+                        *(const float4 *)(st + row * RA + 16 * (ch ^ ring::swz_a<RA>(row)));
+                    const float4 hi =
+                        *(const float4 *)(st + row * RA + 16 * ((ch + 1) ^ ring::swz_a<RA>(row)));
+                    const float uv[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                    v8bf u1, u2, u3;
+                    split3(uv, u1, u2, u3);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) {
+                        auto product = [&](v16f y) __attribute__((always_inline)) -> v16f {
+                            if constexpr (ADAPT == IGEMM_F16) {
+                                y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v2[j], y, 0, 0, 0);
+                                y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v2[j], y, 0, 0, 0);
+                            }
+                            y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u3, v1[j], y, 0, 0, 0);
+                            y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v1[j], y, 0, 0, 0);
+                            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v1[j], y, 0, 0, 0);
+                        };
+                        if (~own == 0) {
+                            acc[i][j] =
+                                __builtin_bit_cast(v16i, product(__builtin_bit_cast(v16f, acc[i][j])));
+                        } else {
+                            v16f y;
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) y[r] = 0.0f;
+                            y = product(y);
+                            // Rows of other adapters keep what they have: nothing of
+                            // this one, infinities and NaN included, reaches them.
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) {
+                                const int old = acc[i][j][r];
+                                const bool it = (own >> M::out_row(lane, r)) & 1;
+                                acc[i][j][r] = it ? as_int(as_float(old) + y[r]) : old;
+                            }
+                        }
+                    }
+                }
+            }
+        }
+    };
     if constexpr (!REG) {
 #pragma unroll
         for (int s = 0; s < NST - 1; ++s) issue(s, s);
+        terms();
+        // (the k loop's first barrier publishes what terms() leaves in LDS)
+        // The adapters' tiles follow tile nkm - 1: with fewer k-tiles than the ring
+        // holds, the empty ones that were issued above are multiplied too.
+        const int nkm = XT ? max(nkt, NST - 1) : nkt;
         int s = 0;
-        for (int kt = 0; kt < nkt; ++kt) {
+        Unit ahead = {0, 0, -2, 0};
+        bool begun = false;  // (the list is there after the first barrier)
+        auto issue_any = [&](int kt, int st) __attribute__((always_inline)) {
+            if (!XT || kt < nkm) {
+                issue(kt, st);
+            } else {
+                if (!begun) ahead = unit_of(0);
+                begun = true;
+                issue_extra(ahead, st);
+                ahead = next(next(ahead));
+            }
+        };
+        for (int kt = 0; kt < nkm; ++kt) {
             // tile kt has landed when at most the NST - 2 later ones are out
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NST - 2) * DPW)
                          : "memory");
-            issue(kt + NST - 1, s == 0 ? NST - 1 : s - 1);
+            issue_any(kt + NST - 1, s == 0 ? NST - 1 : s - 1);
             tile(s);
             s = s == NST - 1 ? 0 : s + 1;
+        }
+        if constexpr (XT) {
+            scale();
+            Unit now = unit_of(0);
+            while (now.which >= 0) {
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NST - 2) * DPW)
+                             : "memory");
+                issue_any(nkm, s == 0 ? NST - 1 : s - 1);
+                tile_extra(now, s);
+                s = s == NST - 1 ? 0 : s + 1;
+                now = next(next(now));
+            }
         }
         // no DMA may land in LDS that is used anew below
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -402,6 +622,7 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int rpad,
             load(va, vb, 0);
             store(va, vb, 0);
         }
+        terms();
         for (int kt = 0; kt < nkt; ++kt) {
             __syncthreads();
             if (kt + 1 < nkt) load(va, vb, kt + 1);
@@ -431,115 +652,121 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int rpad,
     __syncthreads();  // the ring becomes the waves' output blocks
     char *blk = smem + wave * 32 * PITCH;
     if (!busy) return;
-    float sb[TN];
+    if constexpr (!XT) scale();
+    if constexpr (ADAPT != 0 && REG) {
+        // Through registers: from memory as it is needed.
+        // Eight of a row's u from element e. They do not depend on the adapter, so
+        // all blocks' first ones are fetched at once.
+        auto fetch_u = [&](int row, int e, float (&x)[8]) __attribute__((always_inline)) {
+            const float4 *src = (const float4 *)(u + (int64_t)row * rpad + e);
+            const float4 lo = src[0], hi = src[1];
+            x[0] = lo.x;
+            x[1] = lo.y;
+            x[2] = lo.z;
+            x[3] = lo.w;
+            x[4] = hi.x;
+            x[5] = hi.y;
+            x[6] = hi.z;
+            x[7] = hi.w;
+        };
+        const int e1 = 8 * (lane >> 5);
+        int mine[TM], urow[TM];
+        float uf[TM][8];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-        const int c = n0 + wn0 + 32 * j + M::out_col(lane);
-        sb[j] = p.scale_b != nullptr && c < p.n ? p.scale_b[(int64_t)f.group * p.n + c] : 1.0f;
+        for (int i = 0; i < TM; ++i) {
+            mine[i] = arow_id[wm0 + 32 * i + fr];
+            urow[i] = max(arow[wm0 + 32 * i + fr], 0);
+            fetch_u(urow[i], e1, uf[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            // The block's adapters, one after the other: every row is multiplied
+            // with each, and takes its own one's result. (A row of a matrix
+            // product depends on its own row of the left operand alone, so other
+            // rows' values cannot reach it.)
+            uint64_t todo = __ballot(mine[i] >= 0);
+            while (todo != 0) {
+                const int which =
+                    __builtin_amdgcn_readlane(mine[i], __ffsll((unsigned long long)todo) - 1);
+                todo &= ~__ballot(mine[i] == which);
+                const int rank = rank_of(ad, which);
+                v16f y[TN];
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) y[j][r] = 0.0f;
+                for (int e0 = 0; e0 < rank; e0 += 16) {
+                    u32 w[TN][4];
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) {
+                        const int c = min(n0 + wn0 + 32 * j + fr, p.n - 1);
+                        load8((const uint16_t *)ad.up + which * ad.stride_up + c * ad.ld_up,
+                              e0 + e1, ad.rank, rank, w[j]);
+                    }
+                    float uv[8];
+                    if (e0 == 0) {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) uv[q] = uf[i][q];
+                    } else {
+                        fetch_u(urow[i], e0 + e1, uv);
+                    }
+                    v8bf u1, u2, u3;
+                    split3(uv, u1, u2, u3);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) {
+                        if constexpr (ADAPT == IGEMM_BF16) {
+                            const v4u b4 = {w[j][0], w[j][1], w[j][2], w[j][3]};
+                            const v8bf v = __builtin_bit_cast(v8bf, b4);
+                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u3, v, y[j], 0, 0, 0);
+                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v, y[j], 0, 0, 0);
+                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v, y[j], 0, 0, 0);
+                        } else {
+                            // a float16 value is two bf16 parts, exactly
+                            float h[8];
+#pragma unroll
+                            for (int q = 0; q < 8; ++q)
+                                h[q] = from16<IGEMM_F16>((uint16_t)(w[j][q / 2] >> (16 * (q & 1))));
+                            v8bf v1, v2, v3;
+                            split3(h, v1, v2, v3);
+                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v2, y[j], 0, 0, 0);
+                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u3, v1, y[j], 0, 0, 0);
+                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v2, y[j], 0, 0, 0);
+                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v1, y[j], 0, 0, 0);
+                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v1, y[j], 0, 0, 0);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int4 id = *(const int4 *)(arow_id + wm0 + 32 * i + M::out_row(lane, r));
+                    const int ids[4] = {id.x, id.y, id.z, id.w};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) {
+                            const int old = acc[i][j][r + q];
+                            acc[i][j][r + q] =
+                                ids[q] == which ? as_int(as_float(old) + y[j][r + q]) : old;
+                        }
+                }
+            }
+        }
     }
     auto emit = [&](auto type_c) __attribute__((always_inline)) {
         constexpr int T = decltype(type_c)::value;
         constexpr int ES = T == IGEMM_F32 ? 4 : 2, V = 16 / ES, LPR = 32 * JB / V;  // lanes a row
+        constexpr int P = 32 * JB * ES + 16;  // (the pad keeps four rows off one bank)
 #pragma unroll
         for (int ij = 0; ij < TM * (TN / JB); ++ij) {
             const int i = ij / (TN / JB), jb = ij % (TN / JB) * JB;
             const int r0 = wm0 + 32 * i, c0 = n0 + wn0 + 32 * jb;
-            float x[JB][16];
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const float4 s = *(const float4 *)(arow_s + r0 + M::out_row(lane, r));
-                const float sa[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int j = 0; j < JB; ++j)
-                        x[j][r + q] = (float)acc[i][jb + j][r + q] * sa[q] * sb[jb + j];
-            }
-            if constexpr (ADAPT) {
-                // The block's adapters, one after the other: every row is
-                // multiplied with each, and takes its own one's result. (A row
-                // of a matrix product depends on its own row of the left operand
-                // alone, so other rows' values cannot reach it.)
-                const int mine = arow_id[r0 + fr];
-                const int arow_u = max(arow[r0 + fr], 0);
-                uint64_t todo = __ballot(mine >= 0);
-                while (todo != 0) {
-                    const int which =
-                        __builtin_amdgcn_readlane(mine, __ffsll((unsigned long long)todo) - 1);
-                    todo &= ~__ballot(mine == which);
-                    const int rank = rank_of(ad, which);
-                    v16f y[JB];
-#pragma unroll
-                    for (int j = 0; j < JB; ++j)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) y[j][r] = 0.0f;
-                    for (int e0 = 0; e0 < rank; e0 += 16) {
-                        const int e = e0 + 8 * (lane >> 5);
-                        float uv[8] = {};
-                        for (int q = 0; q < ks; ++q) {
-                            const float4 *src =
-                                (const float4 *)(u + ((int64_t)q * p.rows + arow_u) * rpad + e);
-                            const float4 lo = src[0], hi = src[1];
-                            uv[0] += lo.x;
-                            uv[1] += lo.y;
-                            uv[2] += lo.z;
-                            uv[3] += lo.w;
-                            uv[4] += hi.x;
-                            uv[5] += hi.y;
-                            uv[6] += hi.z;
-                            uv[7] += hi.w;
-                        }
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) uv[q] = e + q < rank ? uv[q] : 0.0f;
-                        v8bf u1, u2, u3;
-                        split3(uv, u1, u2, u3);
-#pragma unroll
-                        for (int j = 0; j < JB; ++j) {
-                            const int c = min(c0 + 32 * j + fr, p.n - 1);
-                            u32 w[4];
-                            load8((const uint16_t *)ad.up + which * ad.stride_up + c * ad.ld_up,
-                                  e, ad.rank, rank, w);
-                            if (ad.type == IGEMM_BF16) {
-                                const v4u b4 = {w[0], w[1], w[2], w[3]};
-                                const v8bf v = __builtin_bit_cast(v8bf, b4);
-                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u3, v, y[j], 0, 0, 0);
-                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v, y[j], 0, 0, 0);
-                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v, y[j], 0, 0, 0);
-                            } else {
-                                // a float16 value is two bf16 parts, exactly
-                                float h[8];
-#pragma unroll
-                                for (int q = 0; q < 8; ++q)
-                                    h[q] = from16<IGEMM_F16>((uint16_t)(w[q / 2] >> (16 * (q & 1))));
-                                v8bf v1, v2, v3;
-                                split3(h, v1, v2, v3);
-                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v2, y[j], 0, 0, 0);
-                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u3, v1, y[j], 0, 0, 0);
-                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v2, y[j], 0, 0, 0);
-                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v1, y[j], 0, 0, 0);
-                                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v1, y[j], 0, 0, 0);
-                            }
-                        }
-                    }
-#pragma unroll
-                    for (int r = 0; r < 16; r += 4) {
-                        const int4 id = *(const int4 *)(arow_id + r0 + M::out_row(lane, r));
-                        const int ids[4] = {id.x, id.y, id.z, id.w};
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-#pragma unroll
-                            for (int j = 0; j < JB; ++j)
-                                x[j][r + q] = ids[q] == which ? x[j][r + q] + y[j][r + q]
-                                                              : x[j][r + q];
-                    }
-                }
-            }
-            constexpr int P = 32 * JB * ES + 16;  // (the pad keeps four rows off one bank)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
 #pragma unroll
-                for (int j = 0; j < JB; ++j)
-                    put<T>(blk + M::out_row(lane, r) * P, 32 * j + M::out_col(lane), x[j][r]);
+                for (int j = 0; j < JB; ++j) {
+                    const int x = acc[i][jb + j][r];
+                    put<T>(blk + M::out_row(lane, r) * P, 32 * j + M::out_col(lane), as_float(x));
+                }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
