@@ -338,7 +338,7 @@ Choice choose(int64_t rows, int64_t n, int64_t k, int64_t groups, int64_t adapte
         c.bm = 32, c.bn = 256;
     } else if (avg <= 64 || tiles(128, 128) < num_cu) {
         c.bm = 64, c.bn = 128;
-    } else if (avg >= 192 && adapters == 0 &&
+    } else if (avg >= 192 && (adapters == 0 || rank <= 16) &&
                full(tiles(256, 256), num_cu) >= 0.9 * full(tiles(128, 128), 2 * num_cu)) {
         c.bm = 256, c.bn = 256;
     } else {
@@ -384,8 +384,6 @@ const void *pick_part(bool part) {
 // adapt: the adapters' weight type, 0 for none.
 template <int BM, int BN, int WM, int WN, int NST, int OCC, bool REG>
 const void *pick_epi(bool part, int adapt) {
-    if constexpr (BM == 256)  // (with adapters its registers spill)
-        return adapt == 0 ? pick_part<BM, BN, WM, WN, NST, OCC, REG, 0>(part) : nullptr;
     return adapt == 0            ? pick_part<BM, BN, WM, WN, NST, OCC, REG, 0>(part)
            : adapt == IGEMM_BF16 ? pick_part<BM, BN, WM, WN, NST, OCC, REG, IGEMM_BF16>(part)
                                  : pick_part<BM, BN, WM, WN, NST, OCC, REG, IGEMM_F16>(part);
@@ -394,8 +392,9 @@ const void *pick_epi(bool part, int adapt) {
 // 64 rows of 64 experts, 1024 x 2048: 32 x 256 20.5, 32 x 128 23.5; 4096 rows,
 // 2048 x 1024: 64 x 128 43.5, 64 x 256 47.7, 128 x 128 47.9; 32768 rows, 4096 x 2048:
 // 256 x 256 366, 128 x 256 400, 128 x 128 430; one weight, 8192 x 11008 x 4096: 367,
-// 397, 388, with adapters of rank 16 430, 458, 432; 2048 x 4096 x 4096, 128 tiles of
-// 256 x 256: 57, else 40.)
+// 397, 388, with adapters of rank 16 416, 458, 422, of rank 64 552, 535, 514 (two waves a
+// SIMD have no other work while the adapters' tiles arrive); 2048 x 4096 x 4096, 128
+// tiles of 256 x 256: 57, else 40.)
 const void *pick(int bm, int bn, bool reg, bool part, int adapt, int *threads) {
     *threads = bm == 256 ? 512 : 256;
     if (reg)

@@ -581,35 +581,45 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
         // holds, the empty ones that were issued above are multiplied too.
         const int nkm = XT ? max(nkt, NST - 1) : nkt;
         int s = 0;
-        Unit ahead = {0, 0, -2, 0};
-        bool begun = false;  // (the list is there after the first barrier)
-        auto issue_any = [&](int kt, int st) __attribute__((always_inline)) {
-            if (!XT || kt < nkm) {
-                issue(kt, st);
-            } else {
-                if (!begun) ahead = unit_of(0);
-                begun = true;
-                issue_extra(ahead, st);
-                ahead = next(next(ahead));
-            }
-        };
-        for (int kt = 0; kt < nkm; ++kt) {
+        auto arrived = [&]() __attribute__((always_inline)) {
             // tile kt has landed when at most the NST - 2 later ones are out
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NST - 2) * DPW)
                          : "memory");
-            issue_any(kt + NST - 1, s == 0 ? NST - 1 : s - 1);
-            tile(s);
-            s = s == NST - 1 ? 0 : s + 1;
-        }
-        if constexpr (XT) {
+        };
+        auto turn = [&]() __attribute__((always_inline)) { s = s == NST - 1 ? 0 : s + 1; };
+        if constexpr (!XT) {
+            for (int kt = 0; kt < nkm; ++kt) {
+                arrived();
+                issue(kt + NST - 1, s == 0 ? NST - 1 : s - 1);
+                tile(s);
+                turn();
+            }
+        } else {
+            // (the last tiles apart: what only they need is not kept over the others)
+            int kt = 0;
+            for (; kt < nkm - (NST - 1); ++kt) {
+                arrived();
+                issue(kt + NST - 1, s == 0 ? NST - 1 : s - 1);
+                tile(s);
+                turn();
+            }
+            Unit ahead = {0, 0, -2, 0};
+            for (int x = 0; x < NST - 1; ++x) {
+                arrived();
+                if (x == 0) ahead = unit_of(0);  // (listed before this barrier)
+                issue_extra(ahead, s == 0 ? NST - 1 : s - 1);
+                ahead = next(next(ahead));
+                tile(s);
+                turn();
+            }
             scale();
             Unit now = unit_of(0);
             while (now.which >= 0) {
-                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NST - 2) * DPW)
-                             : "memory");
-                issue_any(nkm, s == 0 ? NST - 1 : s - 1);
+                arrived();
+                issue_extra(ahead, s == 0 ? NST - 1 : s - 1);
+                ahead = next(next(ahead));
                 tile_extra(now, s);
-                s = s == NST - 1 ? 0 : s + 1;
+                turn();
                 now = next(next(now));
             }
         }
