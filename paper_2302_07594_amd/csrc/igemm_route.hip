@@ -51,6 +51,55 @@ __device__ __forceinline__ int below_me(uint64_t mask) {
     return __builtin_amdgcn_mbcnt_hi((u32)(mask >> 32), __builtin_amdgcn_mbcnt_lo((u32)mask, 0));
 }
 
+// Wave-wide maximum and sum by data-parallel moves: within pairs, quads, halves of a
+// row of 16, rows, then a row's last lane to the next row and the half's to the
+// next half; lane 63 has it all. (Exchanges through LDS take an address and a wait
+// each.)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u32 moved(u32 x) {
+    return (u32)__builtin_amdgcn_update_dpp((int)x, (int)x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float max_step(float x) {
+    return fmaxf(x, __builtin_bit_cast(float, moved<CTRL, ROWS>(__builtin_bit_cast(u32, x))));
+}
+__device__ __forceinline__ float wave_max(float x) {
+    x = max_step<0xb1, 0xf>(x);   // lanes 1 0 3 2 of a quad
+    x = max_step<0x4e, 0xf>(x);   // 2 3 0 1
+    x = max_step<0x141, 0xf>(x);  // mirror of half a row
+    x = max_step<0x140, 0xf>(x);  // mirror of a row
+    x = max_step<0x142, 0xa>(x);  // lane 15 of a row to the next (rows 1 and 3)
+    x = max_step<0x143, 0xc>(x);  // lane 31 to rows 2 and 3
+    return __builtin_bit_cast(
+        float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double sum_step(double x) {
+    // rows that are not written add 0
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const u32 lo = (u32)__builtin_amdgcn_update_dpp(0, (int)(u32)b, CTRL, ROWS, 0xf, false);
+    const u32 hi = (u32)__builtin_amdgcn_update_dpp(0, (int)(u32)(b >> 32), CTRL, ROWS, 0xf, false);
+    return x + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum(double x) {
+    x = sum_step<0xb1, 0xf>(x);
+    x = sum_step<0x4e, 0xf>(x);
+    x = sum_step<0x141, 0xf>(x);
+    x = sum_step<0x140, 0xf>(x);
+    x = sum_step<0x142, 0xa>(x);
+    x = sum_step<0x143, 0xc>(x);
+    return read_lane(x, 63);
+}
+
+// 1 / x for x from 1e-290 to 1e290: the hardware's estimate and two Newton steps, within two
+// units of the last place (the compiler's division, three times the instructions, also
+// covers what x cannot be here).
+__device__ __forceinline__ double reciprocal(double x) {
+    double r = __builtin_amdgcn_rcp(x);
+    r = fma(fma(-x, r, 1.0), r, r);
+    return fma(fma(-x, r, 1.0), r, r);
+}
+
 template <bool WIDE>
 struct KeyOf {
     typedef u32 type;
@@ -76,20 +125,36 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-template <int V, int T, bool WIDE>
-__device__ void route_token(const igemm_route_desc &d, int64_t t, const void *__restrict__ logits,
-                            int64_t ld, const float *__restrict__ bias, int32_t *__restrict__ ids,
-                            float *__restrict__ weights, Scratch<V, WIDE> &sc) {
+// A token's logits: expert 64 v + lane in x[v]. Every lane loads, a clamped place if
+// need be: a load under a branch is waited for before the next one is issued.
+template <int V, int T>
+__device__ __forceinline__ void load_token(const igemm_route_desc &d, int64_t t,
+                                           const void *__restrict__ logits, int64_t ld,
+                                           float (&x)[V]) {
+    const int lane = threadIdx.x & 63;
+    const int64_t at = min(t, d.tokens - 1) * ld;
+    float y[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) y[v] = get<T>(logits, at + min(64 * v + lane, d.experts - 1));
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        x[v] = 64 * v + lane < d.experts ? y[v] : -__builtin_huge_valf();
+}
+
+// Returns the lane's chosen expert, or -1.
+template <int V, bool WIDE>
+__device__ int route_token(const igemm_route_desc &d, int64_t t, const float (&l_in)[V],
+                           const float *__restrict__ bias, int32_t *__restrict__ ids,
+                           float *__restrict__ weights, Scratch<V, WIDE> &sc) {
     typedef typename KeyOf<WIDE>::type key_t;
-    constexpr int BITS = sizeof(key_t) * 8;
+    constexpr int BITS = (int)sizeof(key_t) * 8;
     const float none = -__builtin_huge_valf();
     const int lane = threadIdx.x & 63;
     float l[V];
     key_t key[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int e = 64 * v + lane;
-        const float x = e < d.experts ? get<T>(logits, t * ld + e) : none;
+        const float x = l_in[v];
         // (x + 0: no -0)
         l[v] = x == x ? fminf(x, 3.402823466e38f) + 0.0f : none;
     }
@@ -100,38 +165,46 @@ __device__ void route_token(const igemm_route_desc &d, int64_t t, const void *__
         top = none;
 #pragma unroll
         for (int v = 0; v < V; ++v) top = fmaxf(top, l[v]);
-#pragma unroll
-        for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
+        top = wave_max(top);
         total = 0.0;
     }
     auto score = [&](float x) -> double {  // before the division by total
-        return d.score == IGEMM_SOFTMAX ? exp((double)x - (double)top)
-                                        : 1.0 / (1.0 + exp(-(double)x));
+        if (d.score == IGEMM_SOFTMAX) return exp((double)x - (double)top);
+        // (beyond -709 exp overflows and the score is 0)
+        return x > -709.0f ? reciprocal(1.0 + exp(-(double)x)) : 0.0;
     };
     if constexpr (WIDE) {
         double s[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            s[v] = l[v] > none ? score(l[v]) : 0.0;
+            const double x = score(l[v] > none ? l[v] : 0.0f);
+            s[v] = l[v] > none ? x : 0.0;
             if (d.score == IGEMM_SOFTMAX) total += s[v];
         }
         if (d.score == IGEMM_SOFTMAX) {
-#pragma unroll
-            for (int x = 32; x > 0; x /= 2) total += __shfl_xor(total, x);
+            total = wave_sum(total);
             if (total == 0.0) total = 1.0;
         }
+        const double share = reciprocal(total);
+        float b[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) b[v] = 0.0f;
+        if (bias != nullptr)
+#pragma unroll
+            for (int v = 0; v < V; ++v) b[v] = bias[min(64 * v + lane, d.experts - 1)];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const double k =
-                s[v] / total + (bias != nullptr && l[v] > none ? (double)bias[64 * v + lane] : 0.0);
+            const double k = s[v] * share + (double)b[v];
             key[v] = l[v] > none && k > -__builtin_huge_val() ? ordered(k + 0.0) : 0;
         }
     } else {
         if (all && d.score == IGEMM_SOFTMAX) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) total += l[v] > none ? score(l[v]) : 0.0;
-#pragma unroll
-            for (int x = 32; x > 0; x /= 2) total += __shfl_xor(total, x);
+            for (int v = 0; v < V; ++v) {
+                const double x = score(l[v] > none ? l[v] : 0.0f);
+                total += l[v] > none ? x : 0.0;
+            }
+            total = wave_sum(total);
             if (total == 0.0) total = 1.0;
         }
 #pragma unroll
@@ -141,6 +214,7 @@ __device__ void route_token(const igemm_route_desc &d, int64_t t, const void *__
     // ---- groups -----------------------------------------------------------------
     if (d.groups > 1) {
         const int size = d.experts / d.groups;
+        const float per_size = 1.0f / (float)size;
         int per = 1, lg = 0;  // lanes a group: a power of two
         while (2 * per * d.groups <= 64) per *= 2, ++lg;
 #pragma unroll
@@ -174,26 +248,48 @@ __device__ void route_token(const igemm_route_desc &d, int64_t t, const void *__
         const uint64_t kept = __ballot(g < d.groups && mine != 0 && rank < d.top_groups);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int x = min((64 * v + lane) / size, d.groups - 1);
+            // (experts and sizes up to 1024: the product is far from any integer)
+            const int x = min((int)((64 * v + lane + 0.5f) * per_size), d.groups - 1);
             if (!((kept >> (x << lg)) & 1)) key[v] = 0;
         }
     }
 
     // ---- the top_k --------------------------------------------------------------
-    auto reach = [&](key_t th) -> int {
+    // The search runs on the keys' high words and goes on to the low ones only if
+    // these leave more than top_k of them.
+    u32 hi[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) hi[v] = (u32)(key[v] >> (BITS - 32));
+    auto reach = [&](u32 th) -> int {
         int c = 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v) c += __popcll(__ballot(key[v] >= th));
+        for (int v = 0; v < V; ++v) c += __popcll(__ballot(hi[v] >= th));
         return c;
     };
+    // (every key above 0 has a high word above 0)
     const int k = min(d.top_k, reach(1));
     key_t th = 0;
     if (k > 0) {
-        for (int b = BITS - 1; b >= 0; --b) {
-            const key_t next = th | ((key_t)1 << b);
-            const int c = reach(next);
-            if (c >= k) th = next;
-            if (c == k) break;
+        u32 th_hi = 0;
+        int c = 0;
+        for (int b = 31; b >= 0; --b) {
+            const u32 next = th_hi | 1u << b;
+            const int n = reach(next);
+            if (n >= k) th_hi = next, c = n;
+            if (n == k) break;
+        }
+        th = (key_t)th_hi << (BITS - 32);
+        if constexpr (WIDE) {
+            if (c != k) {
+                for (int b = 31; b >= 0; --b) {
+                    const key_t next = th | (key_t)1 << b;
+                    int n = 0;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) n += __popcll(__ballot(key[v] >= next));
+                    if (n >= k) th = next;
+                    if (n == k) break;
+                }
+            }
         }
     }
     // keys above th, and of those equal to it the first ones that still fit
@@ -224,11 +320,9 @@ __device__ void route_token(const igemm_route_desc &d, int64_t t, const void *__
     const float x = mine ? sc.logit[lane] : none;
     const int index = mine ? sc.index[lane] : -1;
     if (!all && d.score == IGEMM_SOFTMAX) {
-        top = x;  // the largest logit is among the chosen
-#pragma unroll
-        for (int o = 32; o > 0; o /= 2) top = fmaxf(top, __shfl_xor(top, o));
+        top = wave_max(x);  // the largest logit is among the chosen
     }
-    const double s = mine ? score(x) / total : 0.0;
+    const double s = mine ? score(x) * reciprocal(total) : 0.0;
     int rank = 0;
     double sum = 0.0;
     for (int j = 0; j < k; ++j) {
@@ -237,13 +331,14 @@ __device__ void route_token(const igemm_route_desc &d, int64_t t, const void *__
         sum += read_lane(s, j);
     }
     double w = s;
-    if (d.renormalise) w = sum > 0.0 ? s / sum : 0.0;
+    if (d.renormalise) w = sum > 1e-290 ? s * reciprocal(sum) : sum > 0.0 ? s / sum : 0.0;
     if (lane < d.top_k) {
         const int at = mine ? rank : lane;
         ids[t * d.top_k + at] = index;
         weights[t * d.top_k + at] = mine ? (float)(w * (double)d.scale) : 0.0f;
     }
     wave_sync();  // (the scratch is the next token's)
+    return index;
 }
 
 // ---- the plan -------------------------------------------------------------------
@@ -343,14 +438,36 @@ __device__ void plan_alone(const int32_t *ids, int slots, int experts, int32_t *
 
 // ---- kernels ----------------------------------------------------------------------
 
+// `each` tokens a wave, one after the other. counts (null: none wanted): the
+// workgroup's slots of each expert go to counts[block][expert].
+constexpr int kWaves = 16;
 template <int V, int T, bool WIDE>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kWaves * 64)
 route_tokens(igemm_route_desc d, const void *__restrict__ logits, int64_t ld,
-             const float *__restrict__ bias, int32_t *ids, float *weights) {
-    __shared__ Scratch<V, WIDE> sc[4];
+             const float *__restrict__ bias, int32_t *ids, float *weights, int each,
+             int32_t *__restrict__ counts) {
+    __shared__ Scratch<V, WIDE> sc[kWaves];
+    __shared__ int count[64 * V];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t t = (int64_t)blockIdx.x * 4 + wave;
-    if (t < d.tokens) route_token<V, T, WIDE>(d, t, logits, ld, bias, ids, weights, sc[wave]);
+    if (counts != nullptr) {
+        for (int e = threadIdx.x; e < d.experts; e += kWaves * 64) count[e] = 0;
+        __syncthreads();
+    }
+    int64_t t = (int64_t)blockIdx.x * kWaves * each + wave;
+    float l[V], ahead[V];
+    load_token<V, T>(d, t, logits, ld, ahead);
+    for (int x = 0; x < each && t < d.tokens; ++x, t += kWaves) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) l[v] = ahead[v];
+        if (x + 1 < each) load_token<V, T>(d, t + kWaves, logits, ld, ahead);
+        const int id = route_token<V, WIDE>(d, t, l, bias, ids, weights, sc[wave]);
+        if (counts != nullptr && id >= 0) atomicAdd(&count[id], 1);
+    }
+    if (counts != nullptr) {
+        __syncthreads();
+        for (int e = threadIdx.x; e < d.experts; e += kWaves * 64)
+            counts[blockIdx.x * d.experts + e] = count[e];
+    }
 }
 
 // A few tokens: one workgroup routes them, a wave each, and makes the plan.
@@ -366,8 +483,11 @@ route_few(igemm_route_desc d, const void *__restrict__ logits, int64_t ld,
     } m;
     __shared__ int start[64 * V], waves[kFewWaves];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for (int t = wave; t < d.tokens; t += kFewWaves)
-        route_token<V, T, WIDE>(d, t, logits, ld, bias, ids, weights, m.sc[wave]);
+    for (int t = wave; t < d.tokens; t += kFewWaves) {
+        float l[V];
+        load_token<V, T>(d, t, logits, ld, l);
+        route_token<V, WIDE>(d, t, l, bias, ids, weights, m.sc[wave]);
+    }
     __syncthreads();
     plan_alone<kFewWaves>(ids, (int)d.tokens * d.top_k, d.experts, offsets, order, start, m.count,
                           waves);
@@ -381,40 +501,39 @@ plan_one(const int32_t *ids, int slots, int experts, int32_t *offsets, int32_t *
     plan_alone<kPlanWaves>(ids, slots, experts, offsets, order, start, count, waves);
 }
 
-// Many slots: `chunk` of them a workgroup, whose counts of each expert go to
-// counts[block][expert]; then each workgroup places its own after those of the
-// experts and workgroups before.
-__global__ void __launch_bounds__(256)
-plan_counts(const int32_t *__restrict__ ids, int slots, int experts, int chunk,
-            int32_t *__restrict__ counts) {
-    __shared__ int start[1024];
-    const int tid = threadIdx.x;
-    for (int e = tid; e < experts; e += 256) start[e] = 0;
-    __syncthreads();
-    const int64_t s0 = (int64_t)blockIdx.x * chunk;
-    const int64_t s1 = min(s0 + chunk, (int64_t)slots);
-    for (int64_t s = s0 + tid; s < s1; s += 256)
-        if (ids[s] >= 0) atomicAdd(&start[ids[s]], 1);
-    __syncthreads();
-    for (int e = tid; e < experts; e += 256) counts[blockIdx.x * experts + e] = start[e];
-}
+// Many slots: `join` of the blocks that route_tokens counted a workgroup, `block` slots
+// each, placed after those of the experts, and of the workgroups, before.
 __global__ void __launch_bounds__(kPlanWaves * 64)
-plan_places(const int32_t *__restrict__ ids, int slots, int experts, int chunk,
-            const int32_t *__restrict__ counts, int32_t *__restrict__ offsets,
+plan_places(const int32_t *__restrict__ ids, int slots, int experts, int block, int blocks,
+            int join, const int32_t *__restrict__ counts, int32_t *__restrict__ offsets,
             int32_t *__restrict__ order) {
     __shared__ int start[1024], before[1024], waves[kPlanWaves];
     __shared__ int count[kPlanWaves * 1024];
-    const int tid = threadIdx.x, blocks = gridDim.x;
-    for (int e = tid; e < experts; e += kPlanWaves * 64) {
-        int mine = 0, all = 0;
-#pragma unroll 8
-        for (int b = 0; b < blocks; ++b) {
-            const int c = counts[b * experts + e];
-            mine += b < (int)blockIdx.x ? c : 0;
-            all += c;
+    const int tid = threadIdx.x, mine = blockIdx.x * join;
+    for (int e = tid; e < experts; e += kPlanWaves * 64) start[e] = before[e] = 0;
+    __syncthreads();
+    // The sums over the blocks by `parts` threads an expert, so that the loads of
+    // all are in flight together.
+    int parts = 1;
+    while (2 * parts * experts <= kPlanWaves * 64) parts *= 2;
+    const int span = (blocks + parts - 1) / parts;
+    for (int x = tid; x < parts * experts; x += kPlanWaves * 64) {
+        const int part = x / experts, e = x - part * experts;
+        const int b0 = part * span, b1 = min(b0 + span, blocks);
+        int low = 0, all = 0;
+        for (int b = b0; b < b1; b += 16) {
+            int c[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) c[i] = counts[min(b + i, b1 - 1) * experts + e];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if (b + i >= b1) c[i] = 0;
+                low += b + i < mine ? c[i] : 0;
+                all += c[i];
+            }
         }
-        start[e] = all;
-        before[e] = mine;
+        atomicAdd(&start[e], all);
+        atomicAdd(&before[e], low);
     }
     __syncthreads();
     const int total = scan_experts<kPlanWaves>(start, experts, waves);
@@ -424,8 +543,8 @@ plan_places(const int32_t *__restrict__ ids, int slots, int experts, int chunk,
     }
     __syncthreads();
     for (int e = tid; e < experts; e += kPlanWaves * 64) start[e] += before[e];
-    const int64_t s0 = (int64_t)blockIdx.x * chunk;
-    const int64_t s1 = min(s0 + chunk, (int64_t)slots);
+    const int64_t s0 = (int64_t)mine * block;
+    const int64_t s1 = min(s0 + (int64_t)join * block, (int64_t)slots);
     for (int64_t s = max((int64_t)total, s0) + tid; s < s1; s += kPlanWaves * 64) order[s] = -1;
     __syncthreads();
     place_slots<kPlanWaves>(ids, (int)s0, (int)s1, experts, start, count, order);
@@ -452,21 +571,21 @@ const void *pick_few(int type, bool wide) {
                                 : (const void *)route_few<V, IGEMM_F16, false>;
 }
 
-// One workgroup places up to this many slots; more are cut into at most kMostBlocks
-// ranges.
-constexpr int64_t kAlone = 8192, kChunk = 2048, kMostBlocks = 128;
-int64_t chunk_of(int64_t slots) {
-    const int64_t c = (slots + kMostBlocks - 1) / kMostBlocks;
-    return c > kChunk ? c : kChunk;
+// One workgroup places up to this many slots; of more, each workgroup places at
+// least kRange.
+constexpr int64_t kAlone = 8192, kRange = 2048;
+// At most 256 workgroups of route_tokens, one a compute unit.
+int64_t tokens_a_block(int64_t tokens) {
+    const int64_t each = (tokens + 256 * kWaves - 1) / (256 * kWaves);
+    return (each > 1 ? each : 1) * kWaves;
 }
 
 }  // namespace
 
 int64_t route_workspace(const igemm_route_desc &d, bool plan) {
-    const int64_t slots = d.tokens * d.top_k;
-    if (!plan || slots <= kAlone) return 0;
-    const int64_t chunk = chunk_of(slots);
-    return ((slots + chunk - 1) / chunk * d.experts * 4 + 255) / 256 * 256;
+    if (!plan || d.tokens * d.top_k <= kAlone) return 0;
+    const int64_t per = tokens_a_block(d.tokens);
+    return ((d.tokens + per - 1) / per * d.experts * 4 + 255) / 256 * 256;
 }
 
 int launch_route(const igemm_route_desc &d, const void *logits, int64_t ld, const float *bias,
@@ -487,27 +606,30 @@ int launch_route(const igemm_route_desc &d, const void *logits, int64_t ld, cons
                    ? IGEMM_OK
                    : IGEMM_EHIP;
     }
+    const int per = (int)tokens_a_block(d.tokens), blocks = (int)((d.tokens + per - 1) / per);
+    const bool alone = slots <= kAlone;
+    int32_t *counts = offsets == nullptr || alone ? nullptr : (int32_t *)workspace;
     if (d.tokens > 0) {
         const void *fn = d.experts <= 64    ? pick<1>(d.type, wide)
                          : d.experts <= 128 ? pick<2>(d.type, wide)
                          : d.experts <= 256 ? pick<4>(d.type, wide)
                          : d.experts <= 512 ? pick<8>(d.type, wide)
                                             : pick<16>(d.type, wide);
-        void *args[] = {&dd, (void *)&logits, &ld, (void *)&bias, &ids, &weights};
-        if (hipLaunchKernel(fn, dim3((unsigned)((d.tokens + 3) / 4)), dim3(256), args, 0,
-                            stream) != hipSuccess)
+        int each = per / kWaves;
+        void *args[] = {&dd,  (void *)&logits, &ld,   (void *)&bias,
+                        &ids, &weights,        &each, &counts};
+        if (hipLaunchKernel(fn, dim3((unsigned)blocks), dim3(kWaves * 64), args, 0, stream) !=
+            hipSuccess)
             return IGEMM_EHIP;
     }
     if (offsets == nullptr) return IGEMM_OK;
-    if (slots <= kAlone) {
+    if (alone) {
         plan_one<<<dim3(1), kPlanWaves * 64, 0, stream>>>(ids, slots, d.experts, offsets, order);
     } else {
-        const int chunk = (int)chunk_of(slots);
-        const unsigned blocks = (unsigned)(((int64_t)slots + chunk - 1) / chunk);
-        int32_t *counts = (int32_t *)workspace;
-        plan_counts<<<dim3(blocks), 256, 0, stream>>>(ids, slots, d.experts, chunk, counts);
-        plan_places<<<dim3(blocks), kPlanWaves * 64, 0, stream>>>(ids, slots, d.experts, chunk,
-                                                                  counts, offsets, order);
+        const int64_t block = (int64_t)per * d.top_k;
+        const int join = block < kRange ? (int)((kRange + block - 1) / block) : 1;
+        plan_places<<<dim3((unsigned)((blocks + join - 1) / join)), kPlanWaves * 64, 0, stream>>>(
+            ids, slots, d.experts, (int)block, blocks, join, counts, offsets, order);
     }
     return hipGetLastError() == hipSuccess ? IGEMM_OK : IGEMM_EHIP;
 }

@@ -72,18 +72,27 @@ shrink_tiles(Product p, Adapters ad, float *__restrict__ u, int rpad) {
             constexpr int S = decltype(set)::value;
             const int k0 = kt * kShrinkTile;
             const int8_t *arow = p.A + (int64_t)min(i0 + (tid >> 4), p.rows - 1) * p.lda;
+            const bool whole = k0 + kShrinkTile <= p.k;  // (no bounds, no branches)
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-                av[S][x] = load_row16(arow, k0 + 256 * x + 16 * (tid & 15), p.k);
+            for (int x = 0; x < 2; ++x) {
+                const int e0 = k0 + 256 * x + 16 * (tid & 15);
+                if (whole) av[S][x] = ring::load_u16((const char *)arow + e0);
+                else av[S][x] = load_row16(arow, e0, p.k);
+            }
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
-                const int r = max(min(r0 + 16 * n + (tid >> 5), rank - 1), 0);
+                const uint16_t *drow =
+                    down + max(min(r0 + 16 * n + (tid >> 5), rank - 1), 0) * ad.ld_down;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    u32 w[4];
-                    load8(down + r * ad.ld_down, min(k0 + 256 * x + 8 * (tid & 31), p.k), p.k, p.k,
-                          w);
-                    dv[S][2 * n + x] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+                    const int e0 = k0 + 256 * x + 8 * (tid & 31);
+                    if (whole) {
+                        dv[S][2 * n + x] = ring::load_u16((const char *)(drow + e0));
+                    } else {
+                        u32 w[4];
+                        load8(drow, min(e0, p.k), p.k, p.k, w);
+                        dv[S][2 * n + x] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+                    }
                 }
             }
         };

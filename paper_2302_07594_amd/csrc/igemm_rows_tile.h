@@ -105,22 +105,30 @@ __device__ void shrink_row(const Product &p, const Adapters &ad, float *__restri
         float s[4] = {};
         for (int k0 = kb; k0 < ke; k0 += 512 * PASS) {
             u32 x[PASS][2], w[4][PASS][4];
+            if (k0 + 512 * PASS <= ke) {
+                // (no bounds, no branches: all in flight together)
 #pragma unroll
-            for (int q = 0; q < PASS; ++q) {
-                const int e0 = min(k0 + 512 * q + 8 * lane, ke);
-                x[q][0] = x[q][1] = 0u;
-                if (e0 + 8 <= ke) {
+                for (int q = 0; q < PASS; ++q) {
+                    const int e0 = k0 + 512 * q + 8 * lane;
                     __builtin_memcpy(x[q], a + e0, 8);
-                } else {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        __builtin_memcpy(w[b][q], down + min(r0 + b, rank - 1) * ad.ld_down + e0, 16);
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < PASS; ++q) {
+                    const int e0 = min(k0 + 512 * q + 8 * lane, ke);
+                    x[q][0] = x[q][1] = 0u;
                     for (int e = 0; e < 8 && e0 + e < ke; ++e) {
                         const u32 b = (u32)(uint8_t)a[e0 + e] << (8 * (e & 3));
                         if (e < 4) x[q][0] |= b;
                         else x[q][1] |= b;
                     }
-                }
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
-                    load8(down + min(r0 + b, rank - 1) * ad.ld_down, e0, p.k, ke, w[b][q]);
+                    for (int b = 0; b < 4; ++b)
+                        load8(down + min(r0 + b, rank - 1) * ad.ld_down, e0, p.k, ke, w[b][q]);
+                }
             }
 #pragma unroll
             for (int q = 0; q < PASS; ++q)
