@@ -174,27 +174,28 @@ __device__ int route_token(const igemm_route_desc &d, int64_t t, const float (&l
         return x > -709.0f ? reciprocal(1.0 + exp(-(double)x)) : 0.0;
     };
     if constexpr (WIDE) {
-        double s[V];
+        // One copy of exp for all registers, through the scratch (rolled: what a wave
+        // runs once costs the fetch of its instructions more than their execution).
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const double x = score(l[v] > none ? l[v] : 0.0f);
-            s[v] = l[v] > none ? x : 0.0;
-            if (d.score == IGEMM_SOFTMAX) total += s[v];
+        for (int v = 0; v < V; ++v) sc.key[64 * v + lane] = __builtin_bit_cast(u32, l[v]);
+        double sum = 0.0;
+#pragma unroll 1
+        for (int e = lane; e < 64 * V; e += 64) {
+            const float x = __builtin_bit_cast(float, (u32)sc.key[e]);
+            const double y = x > none ? score(x) : 0.0;
+            sum += y;
+            sc.key[e] = __builtin_bit_cast(uint64_t, y);
         }
         if (d.score == IGEMM_SOFTMAX) {
-            total = wave_sum(total);
+            total = wave_sum(sum);
             if (total == 0.0) total = 1.0;
         }
         const double share = reciprocal(total);
-        float b[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) b[v] = 0.0f;
-        if (bias != nullptr)
-#pragma unroll
-            for (int v = 0; v < V; ++v) b[v] = bias[min(64 * v + lane, d.experts - 1)];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const double k = s[v] * share + (double)b[v];
+            const float b = bias != nullptr ? bias[min(64 * v + lane, d.experts - 1)] : 0.0f;
+            const double k =
+                __builtin_bit_cast(double, sc.key[64 * v + lane]) * share + (double)b;
             key[v] = l[v] > none && k > -__builtin_huge_val() ? ordered(k + 0.0) : 0;
         }
     } else {
@@ -272,11 +273,12 @@ __device__ int route_token(const igemm_route_desc &d, int64_t t, const float (&l
     if (k > 0) {
         u32 th_hi = 0;
         int c = 0;
-        for (int b = 31; b >= 0; --b) {
+#pragma unroll 1
+        for (int b = 31; b >= 0 && c != k; --b) {
             const u32 next = th_hi | 1u << b;
             const int n = reach(next);
-            if (n >= k) th_hi = next, c = n;
-            if (n == k) break;
+            c = n >= k ? n : c;
+            th_hi = n >= k ? next : th_hi;
         }
         th = (key_t)th_hi << (BITS - 32);
         if constexpr (WIDE) {
@@ -325,6 +327,7 @@ __device__ int route_token(const igemm_route_desc &d, int64_t t, const float (&l
     const double s = mine ? score(x) * reciprocal(total) : 0.0;
     int rank = 0;
     double sum = 0.0;
+#pragma unroll 1
     for (int j = 0; j < k; ++j) {
         const key_t other = read_lane(best, j);
         rank += other > best || (other == best && j < lane);
@@ -440,12 +443,14 @@ __device__ void plan_alone(const int32_t *ids, int slots, int experts, int32_t *
 
 // `each` tokens a wave, one after the other. counts (null: none wanted): the
 // workgroup's slots of each expert go to counts[block][expert].
-constexpr int kWaves = 16;
+// (from 512 experts on, eight waves: their registers)
+constexpr int waves_of(int experts) { return experts <= 256 ? 16 : 8; }
 template <int V, int T, bool WIDE>
-__global__ void __launch_bounds__(kWaves * 64)
+__global__ void __launch_bounds__(waves_of(64 * V) * 64)
 route_tokens(igemm_route_desc d, const void *__restrict__ logits, int64_t ld,
              const float *__restrict__ bias, int32_t *ids, float *weights, int each,
              int32_t *__restrict__ counts) {
+    constexpr int kWaves = waves_of(64 * V);
     __shared__ Scratch<V, WIDE> sc[kWaves];
     __shared__ int count[64 * V];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -465,8 +470,9 @@ route_tokens(igemm_route_desc d, const void *__restrict__ logits, int64_t ld,
     }
     if (counts != nullptr) {
         __syncthreads();
-        for (int e = threadIdx.x; e < d.experts; e += kWaves * 64)
-            counts[blockIdx.x * d.experts + e] = count[e];
+        const int row = (d.experts + 3) & ~3;  // (rows of whole 16 bytes)
+        for (int e = threadIdx.x; e < row; e += kWaves * 64)
+            counts[blockIdx.x * row + e] = e < d.experts ? count[e] : 0;
     }
 }
 
@@ -510,30 +516,32 @@ plan_places(const int32_t *__restrict__ ids, int slots, int experts, int block, 
     __shared__ int start[1024], before[1024], waves[kPlanWaves];
     __shared__ int count[kPlanWaves * 1024];
     const int tid = threadIdx.x, mine = blockIdx.x * join;
+    const int64_t s0 = (int64_t)mine * block;
+    const int64_t s1 = min(s0 + (int64_t)join * block, (int64_t)slots);
     for (int e = tid; e < experts; e += kPlanWaves * 64) start[e] = before[e] = 0;
     __syncthreads();
-    // The sums over the blocks by `parts` threads an expert, so that the loads of
-    // all are in flight together.
+    // The sums over the blocks by `parts` threads for every four experts, so that the
+    // loads of all are in flight together.
+    const int fours = (experts + 3) / 4;
     int parts = 1;
-    while (2 * parts * experts <= kPlanWaves * 64) parts *= 2;
+    while (2 * parts * fours <= kPlanWaves * 64) parts *= 2;
     const int span = (blocks + parts - 1) / parts;
-    for (int x = tid; x < parts * experts; x += kPlanWaves * 64) {
-        const int part = x / experts, e = x - part * experts;
+    for (int x = tid; x < parts * fours; x += kPlanWaves * 64) {
+        const int part = x / fours, q = x - part * fours;
         const int b0 = part * span, b1 = min(b0 + span, blocks);
-        int low = 0, all = 0;
-        for (int b = b0; b < b1; b += 16) {
-            int c[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) c[i] = counts[min(b + i, b1 - 1) * experts + e];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                if (b + i >= b1) c[i] = 0;
-                low += b + i < mine ? c[i] : 0;
-                all += c[i];
-            }
+        v4i low = {0, 0, 0, 0}, all = {0, 0, 0, 0};
+#pragma unroll 8
+        for (int b = b0; b < b1; ++b) {
+            const v4i c = ((const v4i *)counts)[b * fours + q];
+            low += b < mine ? c : v4i{0, 0, 0, 0};
+            all += c;
         }
-        atomicAdd(&start[e], all);
-        atomicAdd(&before[e], low);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (4 * q + i < experts) {
+                atomicAdd(&start[4 * q + i], all[i]);
+                atomicAdd(&before[4 * q + i], low[i]);
+            }
     }
     __syncthreads();
     const int total = scan_experts<kPlanWaves>(start, experts, waves);
@@ -543,8 +551,6 @@ plan_places(const int32_t *__restrict__ ids, int slots, int experts, int block, 
     }
     __syncthreads();
     for (int e = tid; e < experts; e += kPlanWaves * 64) start[e] += before[e];
-    const int64_t s0 = (int64_t)mine * block;
-    const int64_t s1 = min(s0 + (int64_t)join * block, (int64_t)slots);
     for (int64_t s = max((int64_t)total, s0) + tid; s < s1; s += kPlanWaves * 64) order[s] = -1;
     __syncthreads();
     place_slots<kPlanWaves>(ids, (int)s0, (int)s1, experts, start, count, order);
@@ -575,17 +581,17 @@ const void *pick_few(int type, bool wide) {
 // least kRange.
 constexpr int64_t kAlone = 8192, kRange = 2048;
 // At most 256 workgroups of route_tokens, one a compute unit.
-int64_t tokens_a_block(int64_t tokens) {
-    const int64_t each = (tokens + 256 * kWaves - 1) / (256 * kWaves);
-    return (each > 1 ? each : 1) * kWaves;
+int64_t tokens_a_block(int64_t tokens, int experts) {
+    const int64_t waves = waves_of(experts), each = (tokens + 256 * waves - 1) / (256 * waves);
+    return (each > 1 ? each : 1) * waves;
 }
 
 }  // namespace
 
 int64_t route_workspace(const igemm_route_desc &d, bool plan) {
     if (!plan || d.tokens * d.top_k <= kAlone) return 0;
-    const int64_t per = tokens_a_block(d.tokens);
-    return ((d.tokens + per - 1) / per * d.experts * 4 + 255) / 256 * 256;
+    const int64_t per = tokens_a_block(d.tokens, d.experts);
+    return ((d.tokens + per - 1) / per * ((d.experts + 3) / 4) * 16 + 255) / 256 * 256;
 }
 
 int launch_route(const igemm_route_desc &d, const void *logits, int64_t ld, const float *bias,
@@ -606,7 +612,7 @@ int launch_route(const igemm_route_desc &d, const void *logits, int64_t ld, cons
                    ? IGEMM_OK
                    : IGEMM_EHIP;
     }
-    const int per = (int)tokens_a_block(d.tokens), blocks = (int)((d.tokens + per - 1) / per);
+    const int per = (int)tokens_a_block(d.tokens, d.experts), blocks = (int)((d.tokens + per - 1) / per);
     const bool alone = slots <= kAlone;
     int32_t *counts = offsets == nullptr || alone ? nullptr : (int32_t *)workspace;
     if (d.tokens > 0) {
@@ -615,10 +621,11 @@ int launch_route(const igemm_route_desc &d, const void *logits, int64_t ld, cons
                          : d.experts <= 256 ? pick<4>(d.type, wide)
                          : d.experts <= 512 ? pick<8>(d.type, wide)
                                             : pick<16>(d.type, wide);
-        int each = per / kWaves;
+        const int waves = waves_of(d.experts);
+        int each = per / waves;
         void *args[] = {&dd,  (void *)&logits, &ld,   (void *)&bias,
                         &ids, &weights,        &each, &counts};
-        if (hipLaunchKernel(fn, dim3((unsigned)blocks), dim3(kWaves * 64), args, 0, stream) !=
+        if (hipLaunchKernel(fn, dim3((unsigned)blocks), dim3((unsigned)waves * 64), args, 0, stream) !=
             hipSuccess)
             return IGEMM_EHIP;
     }
