@@ -413,7 +413,7 @@ const void *pick(int bm, int bn, bool reg, bool part, int adapt, int *threads) {
                            : pick_epi<128, 128, 64, 64, 2, 2, true>(part, adapt);
     return bm == 32    ? (bn == 256 ? pick_epi<32, 256, 32, 64, 4, 1, false>(part, adapt)
                                     : pick_epi<32, 128, 32, 32, 3, 2, false>(part, adapt))
-           : bm == 64  ? pick_epi<64, 128, 32, 64, 3, 2, false>(part, adapt)
+           : bm == 64  ? pick_epi<64, 128, 32, 64, 2, 3, false>(part, adapt)
            : bm == 128 ? pick_epi<128, 128, 64, 64, 2, 2, false>(part, adapt)
                        : pick_epi<256, 256, 64, 128, 2, 1, false>(part, adapt);
 }
@@ -445,6 +445,11 @@ int launch_product(const Product &p, const Adapters &ad, int num_cu, void *works
     int bm = c.bm, bn = c.bn, threads = 0;
     if (reg && bm >= 64) bn = 128;
     if (reg && bm == 256) bm = 128;
+    // (through registers a workgroup waits more for its loads: 13 experts, 1554 rows,
+    // 1111 x 1777, in 32 rows 20.5 us, in 64 24.0)
+    if (reg && bm == 64 && !sliced &&
+        most_tiles(p.rows, p.groups, 64) * ceil_div(p.n, 128) < 2 * num_cu)
+        bm = 32;
     const void *fn = pick(bm, bn, reg, sliced, adapt ? ad.type : 0, &threads);
     const int64_t first = sliced && adapt ? (int64_t)p.rows * c.ks : 0;
     const int64_t grid = first + most_tiles(p.rows, p.groups, bm) * ceil_div(p.n, bn) * c.slices;

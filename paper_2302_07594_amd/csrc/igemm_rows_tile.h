@@ -236,17 +236,24 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
     const int kbeg = z * kchunk, klen = min(p.k - kbeg, kchunk);
     const int nkt = (klen + BK - 1) / BK;
 
-    for (int r = tid; r < BM; r += NW * 64) {
-        int a = -1, o = -1;
-        if (r < mrows) rows_of(p, f.lo + m0 + r, &a, &o);
-        arow[r] = a;
-        orow[r] = o;
-        if constexpr (ADAPT != 0 && !PART) {
-            const int w = a >= 0 ? ad.ids[a] : -1;
-            arow_id[r] = w >= 0 && w < ad.adapters ? w : -1;
+    // The rows of the tile: the threads that cover them, a wave or two, read the
+    // plan while the others already fetch B.
+    auto fetch_rows = [&]() __attribute__((always_inline)) {
+        for (int r = tid; r < BM; r += NW * 64) {
+            int a = -1, o = -1;
+            if (r < mrows) rows_of(p, f.lo + m0 + r, &a, &o);
+            arow[r] = a;
+            orow[r] = o;
+            if constexpr (ADAPT != 0 && !PART) {
+                const int w = a >= 0 ? ad.ids[a] : -1;
+                arow_id[r] = w >= 0 && w < ad.adapters ? w : -1;
+            }
         }
+    };
+    if constexpr (REG) {
+        fetch_rows();
+        __syncthreads();
     }
-    __syncthreads();
     // What the output needs of each row and column, fetched behind the first
     // k-tiles.
     float sb[TN];
@@ -308,12 +315,14 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
     u32 a_vo[DPA], b_vo[DPB];
     v4u Ars = {0u, 0u, 0u, 0u}, Brs = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int d = 0; d < DPA; ++d) {
-        const int a = arow[a_row[d]];
-        a_vo[d] = a >= 0 ? (u32)a * (u32)lda + 16u * (u32)a_lc[d] : 0x80000000u;
-    }
-#pragma unroll
     for (int d = 0; d < DPB; ++d) b_vo[d] = (u32)b_row[d] * (u32)ldb + 16u * (u32)b_lc[d];
+    auto place_a = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int d = 0; d < DPA; ++d) {
+            const int a = arow[a_row[d]];
+            a_vo[d] = a >= 0 ? (u32)a * (u32)lda + 16u * (u32)a_lc[d] : 0x80000000u;
+        }
+    };
     if constexpr (!REG) {
         // B's resource ends with its k range: rows beyond are zeros, so what A
         // has beyond the range, or in rows with nothing to do, never counts.
@@ -374,20 +383,29 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
             }
         }
     };
-    auto issue = [&](int kt, int s) __attribute__((always_inline)) {
-        const bool in = kt < nkt;
-        v4u ar = Ars, br = Brs;
-        ar.z = in ? ar.z : 0u;
-        br.z = in ? br.z : 0u;
-        const u32 as = in ? (u32)(kt * BK) : 0u;
-        const u32 bs = in ? (u32)(kt * BK) * (u32)ldb : 0u;
+    // k-tile kt into stage s. Tiles past the range are issued too, on empty
+    // resources, so that every wave counts DPB + DPA DMAs a tile.
+    auto issue_b = [&](int kt, int s) __attribute__((always_inline)) {
+        v4u br = Brs;
+        br.z = kt < nkt ? br.z : 0u;
+        const u32 bs = kt < nkt ? (u32)(kt * BK) * (u32)ldb : 0u;
         const u32 base = lds0 + (u32)(s * STAGE);
 #pragma unroll
         for (int d = 0; d < DPB; ++d)
             ring::dma(b_vo[d] + bs, br, base + (u32)(APL + (wave * DPB + d) * 1024));
+    };
+    auto issue_a = [&](int kt, int s) __attribute__((always_inline)) {
+        v4u ar = Ars;
+        ar.z = kt < nkt ? ar.z : 0u;
+        const u32 as = kt < nkt ? (u32)(kt * BK) : 0u;
+        const u32 base = lds0 + (u32)(s * STAGE);
 #pragma unroll
         for (int d = 0; d < DPA; ++d)
             ring::dma(a_vo[d] + as, ar, base + (u32)((wave * DPA + d) * 1024));
+    };
+    auto issue = [&](int kt, int s) __attribute__((always_inline)) {
+        issue_b(kt, s);
+        issue_a(kt, s);
     };
 
     // Through registers: bounded loads of any alignment.
@@ -581,23 +599,35 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
         }
     };
     if constexpr (!REG) {
+        // (the compiler's waits do not know of the DMAs: the rows are read, and waited
+        // for, before this wave's first one)
+        fetch_rows();
 #pragma unroll
-        for (int s = 0; s < NST - 1; ++s) issue(s, s);
+        for (int s = 0; s < NST - 1; ++s) issue_b(s, s);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        place_a();
+#pragma unroll
+        for (int s = 0; s < NST - 1; ++s) issue_a(s, s);
         terms();
         // (the k loop's first barrier publishes what terms() leaves in LDS)
         // The adapters' tiles follow tile nkm - 1: with fewer k-tiles than the ring
         // holds, the empty ones that were issued above are multiplied too.
         const int nkm = XT ? max(nkt, NST - 1) : nkt;
         int s = 0;
-        auto arrived = [&]() __attribute__((always_inline)) {
-            // tile kt has landed when at most the NST - 2 later ones are out
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NST - 2) * DPW)
-                         : "memory");
+        // Tile kt has landed when at most the NST - 2 later ones are out; of the first
+        // tiles, whose A was issued after all of their B, when at most NST - 2 tiles'
+        // A is.
+        auto arrived = [&](int kt) __attribute__((always_inline)) {
+            if (kt < NST - 2)
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NST - 2) * DPA) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NST - 2) * DPW) : "memory");
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         };
         auto turn = [&]() __attribute__((always_inline)) { s = s == NST - 1 ? 0 : s + 1; };
         if constexpr (!XT) {
             for (int kt = 0; kt < nkm; ++kt) {
-                arrived();
+                arrived(kt);
                 issue(kt + NST - 1, s == 0 ? NST - 1 : s - 1);
                 tile(s);
                 turn();
@@ -606,14 +636,14 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
             // (the last tiles apart: what only they need is not kept over the others)
             int kt = 0;
             for (; kt < nkm - (NST - 1); ++kt) {
-                arrived();
+                arrived(kt);
                 issue(kt + NST - 1, s == 0 ? NST - 1 : s - 1);
                 tile(s);
                 turn();
             }
             Unit ahead = {0, 0, -2, 0};
             for (int x = 0; x < NST - 1; ++x) {
-                arrived();
+                arrived(kt + x);
                 if (x == 0) ahead = unit_of(0);  // (listed before this barrier)
                 issue_extra(ahead, s == 0 ? NST - 1 : s - 1);
                 ahead = next(next(ahead));
@@ -623,7 +653,7 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
             scale();
             Unit now = unit_of(0);
             while (now.which >= 0) {
-                arrived();
+                arrived(nkm);
                 issue_extra(ahead, s == 0 ? NST - 1 : s - 1);
                 ahead = next(next(ahead));
                 tile_extra(now, s);
