@@ -16,19 +16,13 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ int byte_of(u32 w, int b) { return (int)(int8_t)(w >> (8 * b)); }
 
-// 16 int8 of a row of `len` from e0, zero beyond it.
-__device__ __forceinline__ v4i load_row16(const int8_t *row, int e0, int len) {
-    if (e0 + 16 <= len) return ring::load_u16((const char *)row + e0);
-    return load_elems<1>(row, e0, len);
-}
-
 // ---- u = scaling scale_a A down^T -------------------------------------------------
 
 // Few rows or few ranks, where the product is not sliced (shrink_row).
 template <int T>
 __global__ void __launch_bounds__(256)
 shrink_rows(Product p, Adapters ad, float *__restrict__ u, int rpad) {
-    shrink_row<4, T>(p, ad, u, rpad, p.k, blockIdx.x, 0);
+    shrink_row<4, T>(p, ad, u, rpad, p.k, blockIdx.x, 0, blockIdx.y);
 }
 
 // Many rows: 32 rows x 16 NR ranks a workgroup, on the matrix cores (int8 values are
@@ -77,7 +71,7 @@ shrink_tiles(Product p, Adapters ad, float *__restrict__ u, int rpad) {
             for (int x = 0; x < 2; ++x) {
                 const int e0 = k0 + 256 * x + 16 * (tid & 15);
                 if (whole) av[S][x] = ring::load_u16((const char *)arow + e0);
-                else av[S][x] = load_row16(arow, e0, p.k);
+                else av[S][x] = ring::load_edge((const char *)arow, e0, p.k, p.k < 16);
             }
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
@@ -90,7 +84,7 @@ shrink_tiles(Product p, Adapters ad, float *__restrict__ u, int rpad) {
                         dv[S][2 * n + x] = ring::load_u16((const char *)(drow + e0));
                     } else {
                         u32 w[4];
-                        load8(drow, min(e0, p.k), p.k, p.k, w);
+                        load8(drow, e0, p.k, p.k, w);
                         dv[S][2 * n + x] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
                     }
                 }
@@ -228,9 +222,12 @@ join_slices(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpa
     if (rank > 0) {
         const uint16_t *up = (const uint16_t *)ad.up + which * ad.stride_up + c * ad.ld_up;
         float y = 0.0f;
+        const bool whole = ad.rank % 8 == 0 && rank % 8 == 0;
+#pragma unroll 2
         for (int r = 0; r < rank; r += 8) {
             u32 w[4];
-            load8(up, r, ad.rank, rank, w);
+            if (whole) __builtin_memcpy(w, up + r, 16);
+            else load8(up, r, ad.rank, rank, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const uint16_t b = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
@@ -439,7 +436,7 @@ int launch_product(const Product &p, const Adapters &ad, int num_cu, void *works
     const bool reg = (uintptr_t)p.A % 4 != 0 || (uintptr_t)p.B % 4 != 0 || p.lda % 4 != 0 ||
                      p.ldb % 4 != 0 || p.stride_b % 4 != 0 ||
                      ((int64_t)p.k + kStepK) * p.ldb > 0xffffffffll ||
-                     (ad.adapters > 0 && c.slices == 1 &&
+                     (ad.adapters > 0 && c.bm == 256 &&
                       ((uintptr_t)ad.up % 4 != 0 || ad.ld_up % 2 != 0 || ad.stride_up % 2 != 0 ||
                        (int64_t)p.rows * c.rpad * 4 > 0x7fffffff));
     int bm = c.bm, bn = c.bn, threads = 0;
@@ -451,15 +448,16 @@ int launch_product(const Product &p, const Adapters &ad, int num_cu, void *works
         most_tiles(p.rows, p.groups, 64) * ceil_div(p.n, 128) < 2 * num_cu)
         bm = 32;
     const void *fn = pick(bm, bn, reg, sliced, adapt ? ad.type : 0, &threads);
-    const int64_t first = sliced && adapt ? (int64_t)p.rows * c.ks : 0;
+    const int64_t first = sliced && adapt ? (int64_t)p.rows * c.ks * (c.rpad / 16) : 0;
     const int64_t grid = first + most_tiles(p.rows, p.groups, bm) * ceil_div(p.n, bn) * c.slices;
     if (fn == nullptr || grid > 0x7fffffff) return IGEMM_ENOTSUP;
     if (adapt && !sliced) {
         if (c.by_row) {
+            const dim3 g((unsigned)p.rows, (unsigned)(c.rpad / 16));
             if (ad.type == IGEMM_BF16)
-                shrink_rows<IGEMM_BF16><<<dim3((unsigned)p.rows), 256, 0, stream>>>(p, ad, u, c.rpad);
+                shrink_rows<IGEMM_BF16><<<g, 256, 0, stream>>>(p, ad, u, c.rpad);
             else
-                shrink_rows<IGEMM_F16><<<dim3((unsigned)p.rows), 256, 0, stream>>>(p, ad, u, c.rpad);
+                shrink_rows<IGEMM_F16><<<g, 256, 0, stream>>>(p, ad, u, c.rpad);
         } else {
             // 32 ranks a workgroup, or 16 where that fills the compute units better.
             const int64_t blocks = ceil_div(p.rows, kShrinkRows);

@@ -54,21 +54,21 @@ __device__ __forceinline__ void split3(const float *x, v8bf &hi, v8bf &mid, v8bf
     }
 }
 
-// 8 consecutive 16-bit values of a row of `len`, from element e0; zero from
-// `used` on.
+// 8 consecutive 16-bit values of a row of `len`, from element e0 >= 0; zero from
+// `used` (<= len) on. No branch but on len: loads under branches wait for each other.
 __device__ __forceinline__ void load8(const uint16_t *row, int e0, int len, int used, u32 w[4]) {
-    if (e0 + 8 <= len) {
-        const v4i v = ring::load_u16((const char *)(row + e0));
+    if (len >= 8) {
+        const v4i v = ring::load_edge((const char *)row, 2 * e0, 2 * len, false);
         w[0] = (u32)v.x;
         w[1] = (u32)v.y;
         w[2] = (u32)v.z;
         w[3] = (u32)v.w;
     } else {
+        u32 x[8];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            w[q] = e0 + 2 * q < len ? row[e0 + 2 * q] : 0u;
-            if (e0 + 2 * q + 1 < len) w[q] |= (u32)row[e0 + 2 * q + 1] << 16;
-        }
+        for (int q = 0; q < 8; ++q) x[q] = row[min(e0 + q, max(len - 1, 0))];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = x[2 * q] | x[2 * q + 1] << 16;
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -86,73 +86,67 @@ __device__ __forceinline__ int rank_of(const Adapters &ad, int which) {
 // kslice) by one workgroup, every wave four ranks at a time, 16 bytes of `down` a
 // lane. What it reads of `down` is one adapter a row, whichever the row's is, so
 // a batch of 16 requests with an adapter each takes as long as one with a shared
-// one. Ranks up to rpad that the adapter does not have are zeros.
+// one. Ranks [r0, r0 + 4 WAVES) of the row; those up to rpad that the adapter does not
+// have are zeros.
 template <int WAVES, int T>
 __device__ void shrink_row(const Product &p, const Adapters &ad, float *__restrict__ u, int rpad,
-                           int kslice, int i, int z) {
+                           int kslice, int i, int z, int block) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int which = ad.ids[i];
-    const int rank = rank_of(ad, which);
-    if (rank == 0) return;
+    const int rank = rank_of(ad, which), r0 = 4 * (block * WAVES + wave);
+    float *row = u + ((int64_t)z * p.rows + i) * rpad;
+    if (r0 >= rank) {  // (the whole wave)
+        if (rank > 0 && lane < 4 && r0 + lane < rpad) row[r0 + lane] = 0.0f;
+        return;
+    }
     const int8_t *a = p.A + (int64_t)i * p.lda;
     float f = p.scale_a != nullptr ? p.scale_a[i] : 1.0f;
     if (ad.scaling != nullptr) f *= ad.scaling[which];
     const uint16_t *down = (const uint16_t *)ad.down + which * ad.stride_down;
     const int kb = z * kslice, ke = min(p.k, kb + kslice);
     constexpr int PASS = 2;  // of 64 lanes x 8 k, all their loads in flight together
-    for (int r0 = 4 * wave; r0 < rank; r0 += 4 * WAVES) {
-        float s[4] = {};
-        for (int k0 = kb; k0 < ke; k0 += 512 * PASS) {
-            u32 x[PASS][2], w[4][PASS][4];
-            if (k0 + 512 * PASS <= ke) {
-                // (no bounds, no branches: all in flight together)
+    float s[4] = {};
+    for (int k0 = kb; k0 < ke; k0 += 512 * PASS) {
+        u32 x[PASS][2], w[4][PASS][4];
+        const bool whole = k0 + 512 * PASS <= ke;
 #pragma unroll
-                for (int q = 0; q < PASS; ++q) {
-                    const int e0 = k0 + 512 * q + 8 * lane;
-                    __builtin_memcpy(x[q], a + e0, 8);
+        for (int q = 0; q < PASS; ++q) {
+            const int e0 = k0 + 512 * q + 8 * lane;
+            if (whole) {
+                __builtin_memcpy(x[q], a + e0, 8);
 #pragma unroll
-                    for (int b = 0; b < 4; ++b)
-                        __builtin_memcpy(w[b][q], down + min(r0 + b, rank - 1) * ad.ld_down + e0, 16);
-                }
+                for (int b = 0; b < 4; ++b)
+                    __builtin_memcpy(w[b][q], down + min(r0 + b, rank - 1) * ad.ld_down + e0, 16);
             } else {
+                const v4i v = ring::load_edge((const char *)a, e0, p.k, p.k < 16);
+                x[q][0] = (u32)v.x;
+                x[q][1] = (u32)v.y;
 #pragma unroll
-                for (int q = 0; q < PASS; ++q) {
-                    const int e0 = min(k0 + 512 * q + 8 * lane, ke);
-                    x[q][0] = x[q][1] = 0u;
-                    for (int e = 0; e < 8 && e0 + e < ke; ++e) {
-                        const u32 b = (u32)(uint8_t)a[e0 + e] << (8 * (e & 3));
-                        if (e < 4) x[q][0] |= b;
-                        else x[q][1] |= b;
-                    }
-#pragma unroll
-                    for (int b = 0; b < 4; ++b)
-                        load8(down + min(r0 + b, rank - 1) * ad.ld_down, e0, p.k, ke, w[b][q]);
-                }
+                for (int b = 0; b < 4; ++b)
+                    load8(down + min(r0 + b, rank - 1) * ad.ld_down, e0, p.k, ke, w[b][q]);
             }
-#pragma unroll
-            for (int q = 0; q < PASS; ++q)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float xe = (float)(int8_t)(x[q][e >> 2] >> (8 * (e & 3)));
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        const uint16_t v = (uint16_t)(w[b][q][e / 2] >> (16 * (e & 1)));
-                        s[b] = fmaf(xe, from16<T>(v), s[b]);
-                    }
-                }
         }
 #pragma unroll
-        for (int o = 32; o > 0; o /= 2)
+        for (int q = 0; q < PASS; ++q)
 #pragma unroll
-            for (int b = 0; b < 4; ++b) s[b] += __shfl_xor(s[b], o);
-        if (lane == 0)
+            for (int e = 0; e < 8; ++e) {
+                const float xe = (float)(int8_t)(x[q][e >> 2] >> (8 * (e & 3)));
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
-                if (r0 + b < rank) u[((int64_t)z * p.rows + i) * rpad + r0 + b] = s[b] * f;
+                for (int b = 0; b < 4; ++b) {
+                    const uint16_t v = (uint16_t)(w[b][q][e / 2] >> (16 * (e & 1)));
+                    s[b] = fmaf(xe, from16<T>(v), s[b]);
+                }
+            }
     }
-    for (int r = rank + threadIdx.x; r < rpad; r += WAVES * 64)
-        u[((int64_t)z * p.rows + i) * rpad + r] = 0.0f;
+#pragma unroll
+    for (int o = 32; o > 0; o /= 2)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) s[b] += __shfl_xor(s[b], o);
+    if (lane == 0)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+            if (r0 + b < rpad) row[r0 + b] = r0 + b < rank ? s[b] * f : 0.0f;
 }
 
 // BM x BN: the workgroup's tile, WM x WN a wave's; NST ring stages; OCC
@@ -160,8 +154,9 @@ __device__ void shrink_row(const Product &p, const Adapters &ad, float *__restri
 // slice z go to part[z][position][column] instead; ADAPT: adapters beside, of this
 // weight type (0: none), u being rows x rpad floats.
 //
-// A sliced product's adapters (PART and ADAPT): the first rows x ks workgroups
-// compute u in ks parts, one a k slice of kshrink (shrink_row), beside the product's.
+// A sliced product's adapters (PART and ADAPT): the first rows x ks x (rank blocks)
+// workgroups compute u in ks parts, one a k slice of kshrink (shrink_row), beside the
+// product's.
 template <int BM, int BN, int WM, int WN, int NST, int OCC, bool REG, bool PART, int ADAPT>
 __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, OCC *((BM / WM) * (BN / WN)) / 4)
 rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, int rpad,
@@ -186,8 +181,8 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
     __shared__ __attribute__((aligned(1024))) char smem[SMEM];
     __shared__ __attribute__((aligned(16))) int arow[BM], orow[BM], arow_id[BM];
     __shared__ __attribute__((aligned(16))) float arow_s[BM];
-    // The adapters of the tile's rows, each once, and their ranks (by DMA only).
-    constexpr bool XT = ADAPT != 0 && !REG && !PART;
+    // The adapters of the tile's rows, each once, and their ranks (256 rows).
+    constexpr bool XT = ADAPT != 0 && !REG && !PART && BM == 256;
     __shared__ int uniq[XT ? BM : 1], uniq_rank[XT ? BM : 1], uniq_n;
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -196,10 +191,11 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
 
     int first = 0;
     if constexpr (PART && ADAPT != 0) {
-        first = p.rows * ks;
+        const int blocks = rpad / (4 * NW);
+        first = p.rows * ks * blocks;
         if ((int)blockIdx.x < first) {
-            shrink_row<NW, ADAPT>(p, ad, u, rpad, kshrink, (int)blockIdx.x % p.rows,
-                           (int)blockIdx.x / p.rows);
+            const int i = (int)blockIdx.x % p.rows, x = (int)blockIdx.x / p.rows;
+            shrink_row<NW, ADAPT>(p, ad, u, rpad, kshrink, i, x / blocks, x % blocks);
             return;
         }
     }
@@ -701,102 +697,122 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
     char *blk = smem + wave * 32 * PITCH;
     if (!busy) return;
     if constexpr (!XT) scale();
-    if constexpr (ADAPT != 0 && REG) {
-        // Through registers: from memory as it is needed.
-        // Eight of a row's u from element e. They do not depend on the adapter, so
-        // all blocks' first ones are fetched at once.
-        auto fetch_u = [&](int row, int e, float (&x)[8]) __attribute__((always_inline)) {
-            const float4 *src = (const float4 *)(u + (int64_t)row * rpad + e);
-            const float4 lo = src[0], hi = src[1];
-            x[0] = lo.x;
-            x[1] = lo.y;
-            x[2] = lo.z;
-            x[3] = lo.w;
-            x[4] = hi.x;
-            x[5] = hi.y;
-            x[6] = hi.z;
-            x[7] = hi.w;
+    if constexpr (ADAPT != 0 && !PART && !XT) {
+        // The adapters from memory: fragments of u and `up` straight into registers, the
+        // next 16 ranks' on their way while these are multiplied (all blocks' first
+        // ones from the start; staged as k-tiles, which is the 256-row tiles' way, 2048 x
+        // 4096 x 4096 with rank 64 took 56 us against 52).
+        struct Piece {
+            float u[8];
+            u32 w[TN][4];
         };
         const int e1 = 8 * (lane >> 5);
-        int mine[TM], urow[TM];
-        float uf[TM][8];
+        int mine[TM], ranks[TM], urow[TM];
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             mine[i] = arow_id[wm0 + 32 * i + fr];
             urow[i] = max(arow[wm0 + 32 * i + fr], 0);
-            fetch_u(urow[i], e1, uf[i]);
+            ranks[i] = rank_of(ad, mine[i]);
+        }
+        auto fetch = [&](int i, int which, int rank, int e0, Piece &f) __attribute__((always_inline)) {
+            const float4 *src = (const float4 *)(u + (int64_t)urow[i] * rpad + e0 + e1);
+            const float4 lo = src[0], hi = src[1];
+            const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+            for (int q = 0; q < 8; ++q) f.u[q] = x[q];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int c = min(n0 + wn0 + 32 * j + fr, p.n - 1);
+                const uint16_t *row =
+                    (const uint16_t *)ad.up + which * ad.stride_up + c * ad.ld_up;
+                if (ad.rank % 8 == 0 && e0 + 16 <= rank)
+                    __builtin_memcpy(f.w[j], row + e0 + e1, 16);
+                else
+                    load8(row, e0 + e1, ad.rank, rank, f.w[j]);
+            }
+        };
+        // The block's adapters, one after the other: every row is multiplied with
+        // each, and takes its own one's result. (A row of a matrix product depends on
+        // its own row of the left operand alone, so other rows' values cannot reach it.)
+        auto first_of = [&](int i, uint64_t todo, int *rank) __attribute__((always_inline)) -> int {
+            const int l = __ffsll((unsigned long long)todo) - 1;
+            *rank = __builtin_amdgcn_readlane(ranks[i], l);
+            return __builtin_amdgcn_readlane(mine[i], l);
+        };
+        Piece head[TM];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const uint64_t todo = __ballot(ranks[i] > 0);
+            if (todo != 0) {
+                int rank;
+                const int which = first_of(i, todo, &rank);
+                fetch(i, which, rank, 0, head[i]);
+            }
         }
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            // The block's adapters, one after the other: every row is multiplied
-            // with each, and takes its own one's result. (A row of a matrix
-            // product depends on its own row of the left operand alone, so other
-            // rows' values cannot reach it.)
-            uint64_t todo = __ballot(mine[i] >= 0);
-            while (todo != 0) {
-                const int which =
-                    __builtin_amdgcn_readlane(mine[i], __ffsll((unsigned long long)todo) - 1);
-                todo &= ~__ballot(mine[i] == which);
-                const int rank = rank_of(ad, which);
-                v16f y[TN];
+            uint64_t todo = __ballot(ranks[i] > 0);
+            if (todo == 0) continue;
+            int rank, e0 = 0, which = first_of(i, todo, &rank);
+            uint64_t own = __ballot(mine[i] == which);
+            todo &= ~own;
+            v16f y[TN];
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) y[j][r] = 0.0f;
-                for (int e0 = 0; e0 < rank; e0 += 16) {
-                    u32 w[TN][4];
-#pragma unroll
-                    for (int j = 0; j < TN; ++j) {
-                        const int c = min(n0 + wn0 + 32 * j + fr, p.n - 1);
-                        load8((const uint16_t *)ad.up + which * ad.stride_up + c * ad.ld_up,
-                              e0 + e1, ad.rank, rank, w[j]);
-                    }
-                    float uv[8];
-                    if (e0 == 0) {
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) uv[q] = uf[i][q];
-                    } else {
-                        fetch_u(urow[i], e0 + e1, uv);
-                    }
-                    v8bf u1, u2, u3;
-                    split3(uv, u1, u2, u3);
-#pragma unroll
-                    for (int j = 0; j < TN; ++j) {
-                        if constexpr (ADAPT == IGEMM_BF16) {
-                            const v4u b4 = {w[j][0], w[j][1], w[j][2], w[j][3]};
-                            const v8bf v = __builtin_bit_cast(v8bf, b4);
-                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u3, v, y[j], 0, 0, 0);
-                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v, y[j], 0, 0, 0);
-                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v, y[j], 0, 0, 0);
-                        } else {
-                            // a float16 value is two bf16 parts, exactly
-                            float h[8];
-#pragma unroll
-                            for (int q = 0; q < 8; ++q)
-                                h[q] = from16<IGEMM_F16>((uint16_t)(w[j][q / 2] >> (16 * (q & 1))));
-                            v8bf v1, v2, v3;
-                            split3(h, v1, v2, v3);
-                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v2, y[j], 0, 0, 0);
-                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u3, v1, y[j], 0, 0, 0);
-                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v2, y[j], 0, 0, 0);
-                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v1, y[j], 0, 0, 0);
-                            y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v1, y[j], 0, 0, 0);
-                        }
-                    }
+                for (int r = 0; r < 16; ++r) y[j][r] = 0.0f;
+            Piece f = head[i];
+            for (;;) {
+                // the next piece: more ranks, or the next adapter's first
+                Piece ahead;
+                const bool more = e0 + 16 < rank, last = !more && todo == 0;
+                int next_which = which, next_rank = rank, next_e0 = e0 + 16;
+                if (!more && todo != 0) {
+                    next_which = first_of(i, todo, &next_rank);
+                    next_e0 = 0;
                 }
+                if (!last) fetch(i, next_which, next_rank, next_e0, ahead);
+                v8bf u1, u2, u3;
+                split3(f.u, u1, u2, u3);
 #pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    const int4 id = *(const int4 *)(arow_id + wm0 + 32 * i + M::out_row(lane, r));
-                    const int ids[4] = {id.x, id.y, id.z, id.w};
+                for (int j = 0; j < TN; ++j) {
+                    const v4u b4 = {f.w[j][0], f.w[j][1], f.w[j][2], f.w[j][3]};
+                    v8bf v1 = __builtin_bit_cast(v8bf, b4), v2;
+                    if constexpr (ADAPT == IGEMM_F16) {
+                        // a float16 value is two bf16 parts, exactly
+                        const v8hf hf = __builtin_bit_cast(v8hf, b4);
+                        float h[8];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
+                        for (int q = 0; q < 8; ++q) h[q] = (float)hf[q];
+                        v8bf rest;
+                        split3(h, v1, v2, rest);
+                        y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v2, y[j], 0, 0, 0);
+                        y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v2, y[j], 0, 0, 0);
+                    }
+                    y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u3, v1, y[j], 0, 0, 0);
+                    y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v1, y[j], 0, 0, 0);
+                    y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v1, y[j], 0, 0, 0);
+                }
+                if (!more) {
+                    // the adapter is done: its rows take the result
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const bool it = (own >> M::out_row(lane, r)) & 1;
 #pragma unroll
                         for (int j = 0; j < TN; ++j) {
-                            const int old = acc[i][j][r + q];
-                            acc[i][j][r + q] =
-                                ids[q] == which ? as_int(as_float(old) + y[j][r + q]) : old;
+                            const int old = acc[i][j][r];
+                            acc[i][j][r] = it ? as_int(as_float(old) + y[j][r]) : old;
+                            y[j][r] = 0.0f;
                         }
+                    }
+                    if (last) break;
+                    own = __ballot(mine[i] == next_which);
+                    todo &= ~own;
                 }
+                which = next_which;
+                rank = next_rank;
+                e0 = next_e0;
+                f = ahead;
             }
         }
     }
