@@ -176,11 +176,11 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
     constexpr int JB = TN < 2 ? TN : 2, PITCH = 32 * JB * 4 + 16;
     constexpr int SMEM = NST * STAGE > NW * 32 * PITCH ? NST * STAGE : NW * 32 * PITCH;
     static_assert(TN % JB == 0, "whole output blocks");
-    static_assert(OCC * (SMEM + 24 * BM + 16) <= 160 * 1024, "LDS");
+    static_assert(OCC * (SMEM + 24 * BM + 4 * BN + 16) <= 160 * 1024, "LDS");
 
     __shared__ __attribute__((aligned(1024))) char smem[SMEM];
     __shared__ __attribute__((aligned(16))) int arow[BM], orow[BM], arow_id[BM];
-    __shared__ __attribute__((aligned(16))) float arow_s[BM];
+    __shared__ __attribute__((aligned(16))) float arow_s[BM], bcol_s[PART ? 4 : BN];
     // The adapters of the tile's rows, each once, and their ranks (256 rows).
     constexpr bool XT = ADAPT != 0 && !REG && !PART && BM == 256;
     __shared__ int uniq[XT ? BM : 1], uniq_rank[XT ? BM : 1], uniq_n;
@@ -252,14 +252,12 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
     }
     // What the output needs of each row and column, fetched behind the first
     // k-tiles.
-    float sb[TN];
     auto terms = [&]() __attribute__((always_inline)) {
         if constexpr (PART) return;
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int c = n0 + wn0 + 32 * j + M::out_col(lane);
-            sb[j] = p.scale_b != nullptr && c < p.n ? p.scale_b[(int64_t)f.group * p.n + c] : 1.0f;
-        }
+        for (int c = tid; c < BN; c += NW * 64)
+            bcol_s[c] = p.scale_b != nullptr && n0 + c < p.n
+                            ? p.scale_b[(int64_t)f.group * p.n + n0 + c]
+                            : 1.0f;
         for (int r = tid; r < BM; r += NW * 64) {
             const int a = arow[r];
             arow_s[r] = a >= 0 && p.scale_a != nullptr ? p.scale_a[a] : 1.0f;
@@ -478,6 +476,10 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+    // B's fragment is the left operand: a lane then holds one row of the block (lane %
+    // 32) and, register by register, columns 8 (r / 4) + 4 (lane / 32) + r % 4, four
+    // consecutive ones that leave in one write; scales and adapters of a row are a
+    // lane's own.
     // A wave whose rows or columns all lie outside leaves the matrix cores to the
     // others (the last row tile of a group is part empty).
     const bool busy = wm0 < mrows && n0 + wn0 < p.n;
@@ -498,23 +500,26 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = M::mma(a[i], b[j], acc[i][j]);
+                for (int j = 0; j < TN; ++j) acc[i][j] = M::mma(b[j], a[i], acc[i][j]);
         }
     };
     // The scaled sums take the places of the raw ones.
     auto scale = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i) {
+            const float sa = arow_s[wm0 + 32 * i + fr];
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const float4 s = *(const float4 *)(arow_s + wm0 + 32 * i + M::out_row(lane, r));
-                const float sa[4] = {s.x, s.y, s.z, s.w};
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
+                for (int r = 0; r < 16; r += 4) {
+                    const float4 s =
+                        *(const float4 *)(bcol_s + wn0 + 32 * j + M::out_row(lane, r));
+                    const float sb[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
-                    for (int j = 0; j < TN; ++j)
-                        acc[i][j][r + q] = as_int((float)acc[i][j][r + q] * sa[q] * sb[j]);
-            }
+                    for (int q = 0; q < 4; ++q)
+                        acc[i][j][r + q] = as_int((float)acc[i][j][r + q] * sa * sb[q]);
+                }
+        }
     };
     auto tile_extra = [&](Unit x, int s) __attribute__((always_inline)) {
         if constexpr (XT) {
@@ -551,7 +556,8 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
                     const int row = wm0 + 32 * i + fr;
-                    const uint64_t own = __ballot(arow_id[row] == which);
+                    const bool it = arow_id[row] == which;
+                    const uint64_t own = __ballot(it);
                     if (own == 0) continue;
                     const int ch = 4 * h + 2 * half;
                     const float4 lo =
@@ -565,12 +571,12 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
                     for (int j = 0; j < TN; ++j) {
                         auto product = [&](v16f y) __attribute__((always_inline)) -> v16f {
                             if constexpr (ADAPT == IGEMM_F16) {
-                                y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v2[j], y, 0, 0, 0);
-                                y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v2[j], y, 0, 0, 0);
+                                y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v2[j], u2, y, 0, 0, 0);
+                                y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v2[j], u1, y, 0, 0, 0);
                             }
-                            y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u3, v1[j], y, 0, 0, 0);
-                            y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v1[j], y, 0, 0, 0);
-                            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v1[j], y, 0, 0, 0);
+                            y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v1[j], u3, y, 0, 0, 0);
+                            y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v1[j], u2, y, 0, 0, 0);
+                            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(v1[j], u1, y, 0, 0, 0);
                         };
                         if (~own == 0) {
                             acc[i][j] =
@@ -585,7 +591,6 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
 #pragma unroll
                             for (int r = 0; r < 16; ++r) {
                                 const int old = acc[i][j][r];
-                                const bool it = (own >> M::out_row(lane, r)) & 1;
                                 acc[i][j][r] = it ? as_int(as_float(old) + y[r]) : old;
                             }
                         }
@@ -679,16 +684,26 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
     if constexpr (PART) {
         int32_t *dst = part + ((int64_t)z * p.rows + f.lo + m0) * p.n + n0;
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i) {
+            const int lr = wm0 + 32 * i + fr;
+            if (lr >= mrows) continue;
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const int c = wn0 + 32 * j + M::out_col(lane);
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int lr = wm0 + 32 * i + M::out_row(lane, r);
-                    if (lr < mrows && n0 + c < p.n) dst[(int64_t)lr * p.n + c] = acc[i][j][r];
+                for (int r = 0; r < 16; r += 4) {
+                    const int c = wn0 + 32 * j + M::out_row(lane, r);
+                    int32_t *at = dst + (int64_t)lr * p.n + c;
+                    const v4i v = {acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2],
+                                   acc[i][j][r + 3]};
+                    if (n0 + c + 4 <= p.n) {
+                        __builtin_memcpy(at, &v, 16);
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            if (n0 + c + q < p.n) at[q] = v[q];
+                    }
                 }
-            }
+        }
         return;
     }
 
@@ -733,7 +748,7 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
         };
         // The block's adapters, one after the other: every row is multiplied with
         // each, and takes its own one's result. (A row of a matrix product depends on
-        // its own row of the left operand alone, so other rows' values cannot reach it.)
+        // its own row of u alone, so other rows' values cannot reach it.)
         auto first_of = [&](int i, uint64_t todo, int *rank) __attribute__((always_inline)) -> int {
             const int l = __ffsll((unsigned long long)todo) - 1;
             *rank = __builtin_amdgcn_readlane(ranks[i], l);
@@ -754,8 +769,7 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
             uint64_t todo = __ballot(ranks[i] > 0);
             if (todo == 0) continue;
             int rank, e0 = 0, which = first_of(i, todo, &rank);
-            uint64_t own = __ballot(mine[i] == which);
-            todo &= ~own;
+            todo &= ~__ballot(mine[i] == which);
             v16f y[TN];
 #pragma unroll
             for (int j = 0; j < TN; ++j)
@@ -786,18 +800,18 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
                         for (int q = 0; q < 8; ++q) h[q] = (float)hf[q];
                         v8bf rest;
                         split3(h, v1, v2, rest);
-                        y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v2, y[j], 0, 0, 0);
-                        y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v2, y[j], 0, 0, 0);
+                        y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v2, u2, y[j], 0, 0, 0);
+                        y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v2, u1, y[j], 0, 0, 0);
                     }
-                    y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u3, v1, y[j], 0, 0, 0);
-                    y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u2, v1, y[j], 0, 0, 0);
-                    y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u1, v1, y[j], 0, 0, 0);
+                    y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v1, u3, y[j], 0, 0, 0);
+                    y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v1, u2, y[j], 0, 0, 0);
+                    y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v1, u1, y[j], 0, 0, 0);
                 }
                 if (!more) {
                     // the adapter is done: its rows take the result
+                    const bool it = mine[i] == which;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const bool it = (own >> M::out_row(lane, r)) & 1;
 #pragma unroll
                         for (int j = 0; j < TN; ++j) {
                             const int old = acc[i][j][r];
@@ -806,8 +820,7 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
                         }
                     }
                     if (last) break;
-                    own = __ballot(mine[i] == next_which);
-                    todo &= ~own;
+                    todo &= ~__ballot(mine[i] == next_which);
                 }
                 which = next_which;
                 rank = next_rank;
@@ -819,17 +832,31 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
     auto emit = [&](auto type_c) __attribute__((always_inline)) {
         constexpr int T = decltype(type_c)::value;
         constexpr int ES = T == IGEMM_F32 ? 4 : 2, V = 16 / ES, LPR = 32 * JB / V;  // lanes a row
-        constexpr int P = 32 * JB * ES + 16;  // (the pad keeps four rows off one bank)
+        // (rows 34 or 68 words apart: a write of 32 rows covers all banks)
+        constexpr int P = 32 * JB * ES + (ES == 2 ? 8 : 16);
 #pragma unroll
         for (int ij = 0; ij < TM * (TN / JB); ++ij) {
             const int i = ij / (TN / JB), jb = ij % (TN / JB) * JB;
             const int r0 = wm0 + 32 * i, c0 = n0 + wn0 + 32 * jb;
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
+            for (int j = 0; j < JB; ++j)
 #pragma unroll
-                for (int j = 0; j < JB; ++j) {
-                    const int x = acc[i][jb + j][r];
-                    put<T>(blk + M::out_row(lane, r) * P, 32 * j + M::out_col(lane), as_float(x));
+                for (int r = 0; r < 16; r += 4) {
+                    float x[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int bits = acc[i][jb + j][r + q];
+                        x[q] = as_float(bits);
+                    }
+                    char *at = blk + fr * P + (32 * j + M::out_row(lane, r)) * ES;
+                    if constexpr (ES == 4) {
+                        *(float4 *)at = make_float4(x[0], x[1], x[2], x[3]);
+                    } else {
+                        uint2 w;
+                        w.x = (u32)to16<T>(x[0]) | (u32)to16<T>(x[1]) << 16;
+                        w.y = (u32)to16<T>(x[2]) | (u32)to16<T>(x[3]) << 16;
+                        *(uint2 *)at = w;
+                    }
                 }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -843,7 +870,9 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
                 const char *src = blk + lr * P + c * ES;
                 char *dst = (char *)p.out + ((int64_t)o * p.ldo + col) * ES;
                 if (col + V <= p.n) {
-                    const v4i v = *(const v4i *)src;
+                    // (src lies at a multiple of 8)
+                    const uint2 lo = *(const uint2 *)src, hi = *(const uint2 *)(src + 8);
+                    const v4i v = {(int)lo.x, (int)lo.y, (int)hi.x, (int)hi.y};
                     __builtin_memcpy(dst, &v, 16);
                 } else {
                     for (int e = 0; col + e < p.n; ++e)
