@@ -350,10 +350,16 @@ Choice choose(int64_t rows, int64_t n, int64_t k, int64_t groups, int64_t adapte
     } else {
         c.bm = 128, c.bn = 128;
     }
-    // Fewer tiles than compute units: narrower ones, then k slices.
+    // Fewer tiles than compute units: narrower and shorter ones, then k slices, with
+    // adapters for few rows only (join_slices reads `up` once a row).
+    c.by_row = adapters > 0 && rank > 0 && rows * rank <= 4096;
+    const bool adapt = adapters > 0 && rank > 0;
     int64_t slices = 1;
     if (c.bm <= 64 && tiles(c.bm, c.bn) < num_cu) {
         c.bn = 128;
+        if (adapt && !c.by_row) c.bm = 32;
+    }
+    if (c.bm <= 64 && tiles(c.bm, c.bn) < num_cu && (!adapt || c.by_row)) {
         const int64_t t = tiles(c.bm, 128);
         if (2 * t <= num_cu) slices = num_cu / t;
         if (slices > k / 256) slices = k / 256;
@@ -365,9 +371,8 @@ Choice choose(int64_t rows, int64_t n, int64_t k, int64_t groups, int64_t adapte
     c.kchunk = (int)chunk;
     c.slices = k > 0 ? (int)ceil_div(k, chunk) : 1;
     if (c.slices > 1) c.part_bytes = up256(c.slices * rows * n * 4);
-    if (adapters > 0 && rank > 0) {
+    if (adapt) {
         c.rpad = (int)(ceil_div(rank, 32) * 32);  // (a row's 32 ranks: one line)
-        c.by_row = c.slices > 1 || rows * rank <= 4096;
         c.ks = c.slices > 1 ? (int)ceil_div(k, kShrinkK) : 1;
         c.u_bytes = up256(c.ks * rows * c.rpad * 4);
     }
