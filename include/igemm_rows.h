@@ -11,8 +11,10 @@
  * before any HIP call, kernels are enqueued on `stream`, the library allocates
  * nothing. What is read on the device (offsets, order, ids, ranks) is not checked
  * on the host: entries out of range choose nothing, and never lead a read or write
- * out of the arrays described here. Values are the same from run to run, bit for
- * bit.
+ * out of the arrays described here. As in igemm.h, elements between the rows of an
+ * int8, down or up matrix, and bytes of the aligned 16 that hold its first or last
+ * element, may be read; their values never matter. Values are the same from run to
+ * run, bit for bit.
  */
 #ifndef IGEMM_ROWS_H
 #define IGEMM_ROWS_H
@@ -118,7 +120,8 @@ int igemm_route(const igemm_route_desc *desc, const void *logits, int64_t ld, co
  * Errors: IGEMM_EINVAL as for igemm_i8, and for slots < 0, scatter not 0 or 1 or
  * an unknown type; IGEMM_ENOTSUP for k beyond 131071 (sums past 2^31), extents
  * beyond 2^31 - 1, more than 65536 groups, an A or a matrix of B within 256 bytes of
- * 2 GiB or over, or 256 rows of out of 2 GiB or more. rows = 0 or n = 0: IGEMM_OK, out unchanged. k = 0: zeros.
+ * 2 GiB or over, 256 rows of out of 2 GiB or more, or a grid of 2^32 threads. rows = 0
+ * or n = 0: IGEMM_OK, out unchanged. k = 0: zeros.
  */
 typedef struct igemm_grouped_desc {
     int64_t rows, n, k, groups;
@@ -146,7 +149,8 @@ int igemm_i8_grouped(const igemm_grouped_desc *desc, const int32_t *offsets,
  *   out      tokens x n, ldo >= n; overwritten; overlaps neither Z nor, unless
  *            it is the same, base.
  * Errors: IGEMM_EINVAL as for igemm_i16 (top_k >= 1); IGEMM_ENOTSUP for n, tokens
- * or top_k beyond 2^31 - 1 or a grid beyond 2^31 - 1 workgroups. tokens = 0 or n = 0: IGEMM_OK.
+ * or top_k beyond 2^31 - 1 or a grid of 2^32 threads (64 GiB of out). tokens = 0 or
+ * n = 0: IGEMM_OK.
  */
 int igemm_combine(int64_t tokens, int64_t top_k, int64_t n, int type, const void *Z, int64_t ldz,
                   const float *weights, const int32_t *ids, const void *base, int64_t ld_base,

@@ -329,6 +329,8 @@ struct Choice {
 
 int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// A grid has fewer than 2^32 threads.
+bool launchable(int64_t blocks, int threads) { return blocks <= 0xffffffffll / threads; }
 
 // By sizes alone, so that the workspace can be sized before the operands exist.
 // What the device will find is taken to be even: `used` groups of `avg` rows.
@@ -455,7 +457,9 @@ int launch_product(const Product &p, const Adapters &ad, int num_cu, void *works
     const void *fn = pick(bm, bn, reg, sliced, adapt ? ad.type : 0, &threads);
     const int64_t first = sliced && adapt ? (int64_t)p.rows * c.ks * (c.rpad / 16) : 0;
     const int64_t grid = first + most_tiles(p.rows, p.groups, bm) * ceil_div(p.n, bn) * c.slices;
-    if (fn == nullptr || grid > 0x7fffffff) return IGEMM_ENOTSUP;
+    if (fn == nullptr || !launchable(grid, threads) ||
+        (adapt && !launchable(ceil_div(p.rows, kShrinkRows), 512)))
+        return IGEMM_ENOTSUP;
     if (adapt && !sliced) {
         if (c.by_row) {
             const dim3 g((unsigned)p.rows, (unsigned)(c.rpad / 16));
@@ -506,7 +510,7 @@ int launch_combine(int64_t tokens, int64_t top_k, int64_t n, int type, const voi
     while (lanes < threads && (int64_t)lanes * vec < n) lanes *= 2;
     int pieces = (int)((n + (int64_t)lanes * vec - 1) / ((int64_t)lanes * vec));
     const int64_t per = threads / lanes, blocks = (tokens * pieces + per - 1) / per;
-    if (tokens * pieces > 0x7fffffff) return IGEMM_ENOTSUP;
+    if (tokens * pieces > 0x7fffffff || !launchable(blocks, threads)) return IGEMM_ENOTSUP;
     const bool wave = lanes >= 64;
 #define IGEMM_COMBINE(t)                                           \
     (wave ? (const void *)combine_slots<t, true> : (const void *)combine_slots<t, false>)

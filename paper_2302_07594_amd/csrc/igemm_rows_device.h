@@ -60,32 +60,36 @@ __device__ __forceinline__ void group_span(const Product &p, int g, int *lo, int
     *cnt = max(b - a, 0);
 }
 // Each lane takes a run of consecutive groups; `mine` are its tiles and `before`
-// the tiles of the lanes below it.
+// the tiles of the lanes below it. Offsets that ascend give fewer than kMostTiles;
+// the sums of others stop there, before they could wrap to a negative number.
+constexpr int kMostTiles = 1 << 27;
 __device__ __forceinline__ int wave_tiles(const Product &p, int bm, int per, int lane,
                                           int *before) {
     int mine = 0;
     for (int g = lane * per; g < min((lane + 1) * per, p.groups); ++g) {
         int lo, cnt;
         group_span(p, g, &lo, &cnt);
-        mine += (cnt + bm - 1) / bm;
+        mine = min(mine + (cnt + bm - 1) / bm, kMostTiles);
     }
     int sum = mine;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
         const int up = __shfl_up(sum, d);
-        if (lane >= d) sum += up;
+        if (lane >= d) sum = min(sum + up, kMostTiles);
     }
     *before = sum - mine;
     return __builtin_amdgcn_readlane(sum, 63);
 }
-// The group that holds row tile t < total.
+// The group that holds row tile t < total; cnt 0 if offsets that do not ascend leave
+// none.
 __device__ __forceinline__ Found wave_find(const Product &p, int bm, int per, int lane, int before,
                                            int t) {
     // the last lane whose tiles begin at or before t and that has any
     int next = __shfl_down(before, 1);
     if (lane == 63) next = 0x7fffffff;
     const uint64_t here = __ballot(before <= t && next > t);
-    const int owner = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)here) - 1);
+    const int owner =
+        __builtin_amdgcn_readfirstlane(max(__ffsll((unsigned long long)here) - 1, 0));
     Found f = {0, __builtin_amdgcn_readlane(before, owner), 0, 0};
     for (int g = owner * per; g < min((owner + 1) * per, p.groups); ++g) {
         int lo, cnt;

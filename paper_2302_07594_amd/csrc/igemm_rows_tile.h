@@ -218,6 +218,7 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
     }
     const int z = (int)(at % slices), t = (int)(at / slices);
     const Found f = wave_find(p, BM, per, lane, before, t / tiles_n);
+    if (f.cnt == 0) return;
     // Within a group: eight row tiles at a time, over all columns.
     int m0, n0;
     {

@@ -217,6 +217,16 @@ def test_tensor_calls_check_their_tensors():
         ig.grouped_i8(a, b, torch.zeros(2, dtype=torch.int32))
 
 
+def test_grids_past_the_largest_are_refused():
+    """A launch of 2^32 threads or more is not supported: named, not a failed launch."""
+    big = 1 << 30
+    assert ig.igemm_combine(big, 1, 4096, 1, P, 4096, Q, None, None, 0, R, 4096, 0) == N
+    d = grouped_desc(rows=(1 << 31) - 1, n=1 << 20, k=1, a_rows=1, out_rows=1, slots=1 << 30)
+    assert call_grouped(d, order=S, ldo=1 << 20, ws=1 << 20, ws_bytes=1 << 62) == N
+    d = adapters_desc(m=1 << 29, n=1, k=1, rank=1)
+    assert call_adapters(d, ws=1 << 20, ws_bytes=1 << 62) == N
+
+
 def test_reference_of_the_gpu_tests_on_hand_cases():
     ids, w, off, order = ref.route(torch.tensor([[0.0, 0.0, -float("inf"), 0.0]]), 3)
     assert ids.tolist() == [[0, 1, 3]] and np.allclose(w, 1 / 3)
