@@ -921,6 +921,8 @@ def _on(device, stream):
             raise TypeError("stream must be None, an int handle or a torch stream")
         if isinstance(stream, int):
             stream = torch.cuda.ExternalStream(stream, device=device)
+        if stream.device != device:
+            raise ValueError("stream must be one of the tensors' device")
         with torch.cuda.stream(stream):
             yield int(stream.cuda_stream)
 
@@ -936,6 +938,9 @@ def _expect(name, what, t, dtypes, shape, device, rows=True):
         raise ValueError(f"{name}: {what} must have shape ({want}), got {tuple(t.shape)}")
     if not t.is_cuda or (device is not None and t.device != device):
         raise ValueError(f"{name}: {what} must be a CUDA (HIP) tensor on the operands' device")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} has no backward pass: call it under torch.no_grad() or detach "
+                         f"{what}")
     if t.numel() == 0:
         return max(t.shape[-1], 1)
     if not rows:
@@ -946,6 +951,13 @@ def _expect(name, what, t, dtypes, shape, device, rows=True):
         raise ValueError(f"{name}: {what} must have unit stride along rows")
     ld = t.stride(-2) if t.dim() > 1 and t.shape[-2] > 1 else max(t.shape[-1], 1)
     return ld
+
+
+def _c_int(name, x) -> int:
+    """An argument that the C call takes as an int (ctypes would wrap a larger one)."""
+    if not -2 ** 31 <= int(x) < 2 ** 31:
+        raise ValueError(f"{name}: {x} does not fit a C int")
+    return int(x)
 
 
 def _space(name, workspace, nbytes, device):
@@ -988,17 +1000,19 @@ def route(logits, top_k, bias=None, groups=1, top_groups=1, group_best=1, score=
         _expect("route", "bias", bias, (torch.float32,), (experts,), logits.device, rows=False)
     if score not in ("softmax", "sigmoid"):
         raise ValueError("route: score must be 'softmax' or 'sigmoid'")
-    desc = RouteDesc(tokens, experts, int(top_k), int(groups), int(top_groups), int(group_best),
+    top_k, groups, top_groups, group_best = \
+        (_c_int("route", x) for x in (top_k, groups, top_groups, group_best))
+    desc = RouteDesc(tokens, experts, top_k, groups, top_groups, group_best,
                      IGEMM_SIGMOID if score == "sigmoid" else IGEMM_SOFTMAX,
                      1 if renormalise else 0, float(scale),
                      _type_of(logits.dtype, "route", "logits"))
     nbytes = igemm_route_query(desc)
     with _on(logits.device, stream) as s:
         new = dict(device=logits.device, dtype=torch.int32)
-        ids = torch.empty((tokens, int(top_k)), **new)
-        weights = torch.empty((tokens, int(top_k)), device=logits.device)
+        ids = torch.empty((tokens, top_k), **new)
+        weights = torch.empty((tokens, top_k), device=logits.device)
         offsets = torch.empty(experts + 1, **new) if plan else None
-        order = torch.empty(tokens * int(top_k), **new) if plan else None
+        order = torch.empty(tokens * top_k, **new) if plan else None
         ws, ws_bytes = _space("route", workspace, nbytes, logits.device)
         st = igemm_route(desc, logits, ld, bias, ids, weights, offsets, order, ws, ws_bytes, s)
     if st != IGEMM_OK:

@@ -14,6 +14,7 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/hip/HIPContextLight.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <pybind11/gil.h>
 #include <torch/csrc/Exceptions.h>
@@ -270,9 +271,10 @@ bool plain_or_none(PyObject *o, at::ScalarType dt, int64_t dim, const at::Tensor
     *t = nullptr;
     if (o == Py_None) return true;
     *t = plain(o, dt, dim);
-    return *t != nullptr;
+    return *t != nullptr && !((*t)->requires_grad() && c10::GradMode::is_enabled());
 }
-// A plain float, bfloat16 or half tensor; its igemm_type in *type.
+// A plain float, bfloat16 or half tensor that no gradient is asked of; its igemm_type
+// in *type.
 const at::Tensor *plain_real(PyObject *o, int64_t dim, int *type) {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::ScalarType dt = THPVariable_Unpack(o).scalar_type();
@@ -280,7 +282,8 @@ const at::Tensor *plain_real(PyObject *o, int64_t dim, int *type) {
     else if (dt == at::kBFloat16) *type = IGEMM_BF16;
     else if (dt == at::kHalf) *type = IGEMM_F16;
     else return nullptr;
-    return plain(o, dt, dim);
+    const at::Tensor *t = plain(o, dt, dim);
+    return t && !(t->requires_grad() && c10::GradMode::is_enabled()) ? t : nullptr;
 }
 // A dense tensor of one or two dimensions of these extents (null: fine).
 bool dense(const at::Tensor *t, int64_t d0, int64_t d1 = -1) {
@@ -420,13 +423,14 @@ PyObject *grouped(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
 // combine(Z, weights, ids, base, out) -> None or a status
 PyObject *combine(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
-    int type, st;
+    int type, w_type, out_type, st;
     const at::Tensor *z = nargs == 5 ? plain_real(args[0], 2, &type) : nullptr;
-    const at::Tensor *w = z ? plain(args[1], at::kFloat, 2) : nullptr, *ids, *base;
-    const at::Tensor *out = w ? plain(args[4], z->scalar_type(), 2) : nullptr;
+    const at::Tensor *w = z ? plain_real(args[1], 2, &w_type) : nullptr, *ids, *base;
+    const at::Tensor *out = w ? plain_real(args[4], 2, &out_type) : nullptr;
     int64_t ldz, ld_base = 0, ldo;
     void *stream;
-    if (!out || modes_active() || !plain_or_none(args[2], at::kInt, 2, &ids) ||
+    if (!out || modes_active() || w_type != IGEMM_F32 || out_type != type ||
+        !plain_or_none(args[2], at::kInt, 2, &ids) ||
         !plain_or_none(args[3], z->scalar_type(), 2, &base) || z->numel() == 0)
         Py_RETURN_NONE;
     const int64_t tokens = w->size(0), top_k = w->size(1), n = z->size(1);
@@ -454,13 +458,14 @@ PyObject *adapters(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     const at::Tensor *b = a ? plain(args[1], at::kChar, 2) : nullptr;
     const at::Tensor *ids = b ? plain(args[2], at::kInt, 1) : nullptr;
     const at::Tensor *down = ids ? plain_real(args[3], 3, &d.weight_type) : nullptr;
-    const at::Tensor *up = down ? plain(args[4], down->scalar_type(), 3) : nullptr;
+    int up_type;
+    const at::Tensor *up = down ? plain_real(args[4], 3, &up_type) : nullptr;
     const at::Tensor *out = up ? plain_real(args[9], 2, &d.type) : nullptr;
     const at::Tensor *sa, *sb, *ranks, *scaling;
     int64_t lda, ldb, ldo, ldd, ldu, stride_d, stride_u;
     int st;
     void *stream;
-    if (!out || modes_active() || d.weight_type == IGEMM_F32 ||
+    if (!out || modes_active() || d.weight_type == IGEMM_F32 || up_type != d.weight_type ||
         !plain_or_none(args[5], at::kFloat, 1, &sa) ||
         !plain_or_none(args[6], at::kFloat, 1, &sb) ||
         !plain_or_none(args[7], at::kInt, 1, &ranks) ||

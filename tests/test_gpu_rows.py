@@ -615,6 +615,48 @@ def test_refusals_leave_the_output_alone():
     assert bool((out == 7).all())
 
 
+def test_no_gradient_is_dropped_in_silence():
+    """A float operand whose gradient would be wanted is refused, and taken where none
+    is recorded."""
+    layer = Layer(8)
+    k = {}
+    layer(keep=k)
+    a, y = k["x"], torch.empty(8, 192, dtype=BF16, device="cuda")
+    out = torch.zeros(24, 256, dtype=BF16, device="cuda")
+    sa = k["s"]
+    calls = [
+        ("logits", lambda t: ig.route(t, 3)[1], k["logits"]),
+        ("scale_a", lambda t: ig.grouped_i8(a, layer.w1, k["offsets"], k["order"], t, slots=3,
+                                            out=out), sa),
+        ("Z", lambda t: ig.combine(t, k["w"], out=y), k["z"]),
+        ("weights", lambda t: ig.combine(k["z"], t, out=y), k["w"]),
+        ("down", lambda t: ig.adapters_i8(a, layer.w0, layer.ids, t, layer.up, out=y), layer.down),
+        ("up", lambda t: ig.adapters_i8(a, layer.w0, layer.ids, layer.down, t, out=y), layer.up)]
+    for name, call, t in calls:
+        want = call(t).clone()
+        leaf = t.detach().clone().requires_grad_()
+        with pytest.raises(ValueError, match=f"detach {name}"):
+            call(leaf)
+        with torch.no_grad():
+            assert torch.equal(call(leaf), want), name
+
+
+def test_offsets_that_do_not_ascend_stay_inside():
+    """The values are not specified, but nothing beside out is written: here the tiles of
+    the groups together are 2^31 and more."""
+    rows, groups = 1 << 22, 65536
+    a = torch.ones(rows, 1, dtype=torch.int8, device="cuda")
+    b = torch.ones(groups, 1, 1, dtype=torch.int8, device="cuda")
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda").repeat(groups // 2)
+    off = torch.cat([off, off[:1]])
+    whole = torch.full((rows + 128, 1), 7.0, device="cuda")
+    out = whole[64:-64]
+    ig.grouped_i8(a, b, off, out=out)
+    torch.cuda.synchronize()
+    assert bool((whole[:64] == 7).all()) and bool((whole[-64:] == 7).all())
+    assert bool(((out == 1) | (out == 7)).all())
+
+
 def test_plain_calls_take_the_compiled_binding(monkeypatch):
     """What the Python code would do is the same, and plain calls do not reach it."""
     layer = Layer(40)

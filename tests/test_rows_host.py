@@ -227,6 +227,15 @@ def test_grids_past_the_largest_are_refused():
     assert call_adapters(d, ws=1 << 20, ws_bytes=1 << 62) == N
 
 
+def test_arguments_that_c_would_wrap_are_refused(monkeypatch):
+    monkeypatch.setattr(ig, "_expect", lambda name, what, t, *a, **kw: t.shape[-1])
+    monkeypatch.setattr(ig, "_load_native", lambda: type("N", (), {"route": lambda *a: None}))
+    for bad in (dict(top_k=2 ** 32 + 1), dict(groups=2 ** 32 + 1), dict(top_groups=-2 ** 32),
+                dict(group_best=2 ** 31)):
+        with pytest.raises(ValueError, match="does not fit"):
+            ig.route(torch.zeros(4, 8), **(dict(top_k=2) | bad))
+
+
 def test_reference_of_the_gpu_tests_on_hand_cases():
     ids, w, off, order = ref.route(torch.tensor([[0.0, 0.0, -float("inf"), 0.0]]), 3)
     assert ids.tolist() == [[0, 1, 3]] and np.allclose(w, 1 / 3)
