@@ -39,19 +39,27 @@ constexpr int kStepK = 128;
 __device__ __forceinline__ int as_int(float x) { return __builtin_bit_cast(int, x); }
 __device__ __forceinline__ float as_float(int x) { return __builtin_bit_cast(float, x); }
 
-// 8 values as bf16 parts hi + mid + lo, each the rounding of what the ones
-// before it leave: 24 bits together. An infinite or NaN value is its hi alone.
+// 8 values as bf16 parts hi + mid + lo, their leading 8 bits, the next 8 and the last 8:
+// the value exactly (cut, not rounded: the largest floats round to infinity in bf16). An
+// infinite or NaN value is its hi alone.
 __device__ __forceinline__ void split3(const float *x, v8bf &hi, v8bf &mid, v8bf &lo) {
+    u32 h[4], m[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const __bf16 h = (__bf16)x[e];
-        const float r = x[e] - (float)h;
-        const bool fine = r == r;
-        const __bf16 m = fine ? (__bf16)r : (__bf16)0.0f;
-        hi[e] = h;
-        mid[e] = m;
-        lo[e] = fine ? (__bf16)(r - (float)m) : (__bf16)0.0f;
+    for (int e = 0; e < 8; e += 2) {
+        u32 top[2], rest[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            top[q] = __builtin_bit_cast(u32, x[e + q]);
+            const float r = x[e + q] - __builtin_bit_cast(float, top[q] & 0xffff0000u);
+            rest[q] = r == r ? __builtin_bit_cast(u32, r) : 0u;
+            lo[e + q] = (__bf16)(__builtin_bit_cast(float, rest[q]) -
+                                 __builtin_bit_cast(float, rest[q] & 0xffff0000u));
+        }
+        h[e / 2] = perm(top[1], top[0], 0x07060302u);
+        m[e / 2] = perm(rest[1], rest[0], 0x07060302u);
     }
+    hi = __builtin_bit_cast(v8bf, h);
+    mid = __builtin_bit_cast(v8bf, m);
 }
 
 // 8 consecutive 16-bit values of a row of `len`, from element e0 >= 0; zero from

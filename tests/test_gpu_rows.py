@@ -427,6 +427,21 @@ def test_adapters_wide_range_of_values():
             check_adapters(A, B, ids, down, up, sa, None, None, None, F32)
 
 
+@pytest.mark.parametrize("wt", [BF16, F16])
+@pytest.mark.parametrize("m, n", [(3, 40), (100, 300), (4096, 4096)])
+def test_adapters_of_the_largest_floats(m, n, wt):
+    """u within half a bf16 step of the largest float, which bf16 would round to infinity."""
+    u, v = float(np.float32(3.4e38)), 2.0 ** -20
+    a = torch.ones(m, 1, dtype=torch.int8, device="cuda")
+    b = torch.zeros(1, n, dtype=torch.int8, device="cuda")
+    ids = torch.zeros(m, dtype=torch.int32, device="cuda")
+    down = torch.ones(1, 1, 1, dtype=wt, device="cuda")
+    up = torch.full((1, n, 1), v, dtype=wt, device="cuda")
+    got = ig.adapters_i8(a, b, ids, down, up, scaling=torch.full((1,), u, device="cuda"),
+                         out_dtype=F32)
+    assert bool((got == u * v).all())
+
+
 def test_projection_without_adapters():
     rng = np.random.default_rng(16)
     for m, n, k in ((1, 4096, 512), (37, 129, 77), (200, 256, 256)):
