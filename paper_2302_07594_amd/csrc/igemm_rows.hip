@@ -44,7 +44,6 @@ shrink_tiles(Product p, Adapters ad, float *__restrict__ u, int rpad) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int i0 = blockIdx.x * kShrinkRows, r0 = blockIdx.y * DR;
-    const int nkt = (p.k + kShrinkTile - 1) / kShrinkTile;
     const int at = i0 + (lane & 31);
     int mine = at < p.rows ? ad.ids[at] : -1;
     if (mine >= ad.adapters) mine = -1;
@@ -60,35 +59,42 @@ shrink_tiles(Product p, Adapters ad, float *__restrict__ u, int rpad) {
         const int rank = rank_of(ad, which);
         const uint16_t *down = (const uint16_t *)ad.down + which * ad.stride_down;
         // Sixteen lanes a row of A, thirty-two a row of `down`. Rows past the end and
-        // ranks past the adapter's read the last one: nothing comes of them.
+        // ranks past the adapter's read the last one: nothing comes of them. Whole
+        // k-tiles are loaded without a branch (behind one, the wait for a tile is a wait
+        // for every load under way), what is left of k at the end.
         v4i av[2][2], dv[2][2 * NR];  // two k-tiles on their way
+        const int8_t *arow = p.A + (int64_t)min(i0 + (tid >> 4), p.rows - 1) * p.lda;
+        const uint16_t *drow[NR];
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+            drow[n] = down + max(min(r0 + 16 * n + (tid >> 5), rank - 1), 0) * ad.ld_down;
         auto load = [&](auto set, int kt) __attribute__((always_inline)) {
             constexpr int S = decltype(set)::value;
-            const int k0 = kt * kShrinkTile;
-            const int8_t *arow = p.A + (int64_t)min(i0 + (tid >> 4), p.rows - 1) * p.lda;
-            const bool whole = k0 + kShrinkTile <= p.k;  // (no bounds, no branches)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int e0 = k0 + 256 * x + 16 * (tid & 15);
-                if (whole) av[S][x] = ring::load_u16((const char *)arow + e0);
-                else av[S][x] = ring::load_edge((const char *)arow, e0, p.k, p.k < 16);
-            }
+            for (int x = 0; x < 2; ++x)
+                av[S][x] = ring::load_u16((const char *)arow + kt * kShrinkTile + 256 * x +
+                                          16 * (tid & 15));
 #pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                const uint16_t *drow =
-                    down + max(min(r0 + 16 * n + (tid >> 5), rank - 1), 0) * ad.ld_down;
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    dv[S][2 * n + x] = ring::load_u16(
+                        (const char *)(drow[n] + kt * kShrinkTile + 256 * x + 8 * (tid & 31)));
+        };
+        auto load_rest = [&](int kt) __attribute__((always_inline)) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                av[0][x] = ring::load_edge((const char *)arow,
+                                           kt * kShrinkTile + 256 * x + 16 * (tid & 15), p.k,
+                                           p.k < 16);
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const int e0 = k0 + 256 * x + 8 * (tid & 31);
-                    if (whole) {
-                        dv[S][2 * n + x] = ring::load_u16((const char *)(drow + e0));
-                    } else {
-                        u32 w[4];
-                        load8(drow, e0, p.k, p.k, w);
-                        dv[S][2 * n + x] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
-                    }
+                    u32 w[4];
+                    load8(drow[n], kt * kShrinkTile + 256 * x + 8 * (tid & 31), p.k, p.k, w);
+                    dv[0][2 * n + x] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
                 }
-            }
         };
         auto store = [&](auto set) __attribute__((always_inline)) {
             constexpr int s = decltype(set)::value;
@@ -111,45 +117,73 @@ shrink_tiles(Product p, Adapters ad, float *__restrict__ u, int rpad) {
         for (int n = 0; n < NR; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[n][e] = 0.0f;
+        auto multiply = [&](auto set) __attribute__((always_inline)) {
+            constexpr int s = decltype(set)::value;
+            // 32 k an instruction: lane group q holds k 8 q .. 8 q + 7 of both.
+            const int row = 16 * rw + c;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                const int chunk = 2 * ks + (q >> 1);
+                const u32 *src = (const u32 *)(sa[s][kg] + row * 128 +
+                                               16 * (chunk ^ (row & 7)) + 8 * (q & 1));
+                const u32 w[2] = {src[0], src[1]};
+                v8s x;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[e] = (short)to16<T>((float)byte_of(w[e >> 2], e & 3));
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                    const v4i d = *(const v4i *)(sd[s][kg] + (16 * n + c) * 256 +
+                                                 16 * ((4 * ks + q) ^ c));
+                    if constexpr (T == IGEMM_BF16)
+                        acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, d), acc[n], 0, 0,
+                            0);
+                    else
+                        acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                            __builtin_bit_cast(v8h, x), __builtin_bit_cast(v8h, d), acc[n], 0, 0,
+                            0);
+                }
+            }
+        };
         if (rank > r0) {
-            load(ic<0>{}, 0);
-            if (nkt > 1) load(ic<1>{}, 1);
-            store(ic<0>{});
-            auto step = [&](auto set, int kt) __attribute__((always_inline)) {
+            const int whole = p.k / kShrinkTile;
+            // k-tile kt from stage s; ahead: the loads of the next but one are issued,
+            // after: the next one goes to the other stage.
+            auto step = [&](auto set, int kt, auto ahead, auto after)
+                __attribute__((always_inline)) {
                 constexpr int s = decltype(set)::value;
                 __syncthreads();
-                if (kt + 2 < nkt) load(ic<s>{}, kt + 2);
-                // 32 k an instruction: lane group q holds k 8 q .. 8 q + 7 of both.
-                const int row = 16 * rw + c;
-#pragma unroll
-                for (int ks = 0; ks < 4; ++ks) {
-                    const int chunk = 2 * ks + (q >> 1);
-                    const u32 *src = (const u32 *)(sa[s][kg] + row * 128 +
-                                                   16 * (chunk ^ (row & 7)) + 8 * (q & 1));
-                    const u32 w[2] = {src[0], src[1]};
-                    v8s x;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        x[e] = (short)to16<T>((float)byte_of(w[e >> 2], e & 3));
-#pragma unroll
-                    for (int n = 0; n < NR; ++n) {
-                        const v4i d = *(const v4i *)(sd[s][kg] + (16 * n + c) * 256 +
-                                                     16 * ((4 * ks + q) ^ c));
-                        if constexpr (T == IGEMM_BF16)
-                            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                __builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, d), acc[n], 0,
-                                0, 0);
-                        else
-                            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                                __builtin_bit_cast(v8h, x), __builtin_bit_cast(v8h, d), acc[n], 0,
-                                0, 0);
-                    }
-                }
-                if (kt + 1 < nkt) store(ic<1 - s>{});
+                if constexpr (decltype(ahead)::value) load(ic<s>{}, kt + 2);
+                multiply(set);
+                if constexpr (decltype(after)::value) store(ic<1 - s>{});
             };
-            for (int kt = 0; kt < nkt; kt += 2) {
-                step(ic<0>{}, kt);
-                if (kt + 1 < nkt) step(ic<1>{}, kt + 1);
+            if (whole > 0) {
+                load(ic<0>{}, 0);
+                load(ic<1>{}, min(1, whole - 1));
+                store(ic<0>{});
+                int kt = 0;
+                for (; kt + 3 < whole; kt += 2) {
+                    step(ic<0>{}, kt, ic<1>{}, ic<1>{});
+                    step(ic<1>{}, kt + 1, ic<1>{}, ic<1>{});
+                }
+                if (whole - kt == 3) {
+                    step(ic<0>{}, kt, ic<1>{}, ic<1>{});
+                    step(ic<1>{}, kt, ic<0>{}, ic<1>{});
+                    step(ic<0>{}, kt, ic<0>{}, ic<0>{});
+                } else if (whole - kt == 2) {
+                    step(ic<0>{}, kt, ic<0>{}, ic<1>{});
+                    step(ic<1>{}, kt, ic<0>{}, ic<0>{});
+                } else {
+                    step(ic<0>{}, kt, ic<0>{}, ic<0>{});
+                }
+            }
+            if (whole * kShrinkTile < p.k) {
+                load_rest(whole);
+                __syncthreads();
+                store(ic<0>{});
+                __syncthreads();
+                multiply(ic<0>{});
             }
         }
         __syncthreads();
