@@ -35,7 +35,7 @@ shrink_rows(Product p, Adapters ad, float *__restrict__ u, int rpad) {
 // where one request ends and the next begins, a block has two.
 constexpr int kShrinkRows = 32, kShrinkTile = 512, kShrinkTurns = 3;
 template <int T, int NR>
-__global__ void __launch_bounds__(512)
+__global__ void __launch_bounds__(512, NR == 1 ? 4 : 2)
 shrink_tiles(Product p, Adapters ad, float *__restrict__ u, int rpad) {
     constexpr int DR = 16 * NR;  // ranks
     __shared__ __attribute__((aligned(16))) char sa[2][4][kShrinkRows * 128];
@@ -82,6 +82,10 @@ shrink_tiles(Product p, Adapters ad, float *__restrict__ u, int rpad) {
                         (const char *)(drow[n] + kt * kShrinkTile + 256 * x + 8 * (tid & 31)));
         };
         auto load_rest = [&](int kt) __attribute__((always_inline)) {
+            // (addresses of the loop over the adapters' every round are not worth
+            // registers all along)
+            int tid = threadIdx.x;
+            asm volatile("" : "+v"(tid));
 #pragma unroll
             for (int x = 0; x < 2; ++x)
                 av[0][x] = ring::load_edge((const char *)arow,
