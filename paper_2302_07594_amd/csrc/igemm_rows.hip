@@ -30,7 +30,9 @@ shrink_rows(Product p, Adapters ad, float *__restrict__ u, int rpad) {
 // 128 k at a time, whose sums meet in LDS at the end. Both operands pass through LDS,
 // read along their rows: fragments read straight from memory take 32 rows a load,
 // which at a row stride of a power of two all lie in one channel of the cache
-// (8192 x 4096, rank 16, 24 adapters: 31 us, against 24 here). The block's adapters are shared
+// (8192 x 4096, rank 16, 24 adapters: 31 us, against 20 here). Bound by
+// the latency of the k-tiles: two are under way, and with 16 ranks two workgroups share
+// a compute unit (at least 8 us of reading A there). The block's adapters are shared
 // out to gridDim.z workgroups, each of which takes its own one after the other:
 // where one request ends and the next begins, a block has two.
 constexpr int kShrinkRows = 32, kShrinkTile = 512, kShrinkTurns = 3;
@@ -219,7 +221,8 @@ shrink_tiles(Product p, Adapters ad, float *__restrict__ u, int rpad) {
 // ---- the slices of few rows joined ---------------------------------------------------
 //
 // A workgroup a position and 256 columns: the raw sums of the k slices added up
-// (exactly), scaled, with the adapter's part in plain float arithmetic.
+// (exactly), scaled, with the adapter's part in plain float arithmetic (`up` is read
+// once a row; 16 x 4096, rank 16: 4.7 us, a launch and two rounds of loads).
 __global__ void __launch_bounds__(256)
 join_slices(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpad,
             const int32_t *__restrict__ part, int slices) {
@@ -280,7 +283,8 @@ join_slices(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpa
 
 // ---- the sum of a token's slots ---------------------------------------------------
 
-// One pass over Z. A thread takes 16 bytes of a row, eight slots' loads at a time
+// One pass over Z, bound by memory (4096 tokens of 8 slots of 4096, bf16: 61 us, 5.5 TB/s;
+// 16 tokens: 4 us, a launch and one round of loads). A thread takes 16 bytes of a row, eight slots' loads at a time
 // before the first is used; a group of `lanes` threads (a power of two) covers a
 // row, or 16 * lanes bytes of it. Slots left out read the token's first slot's
 // row instead, which is at hand, so that no load waits for an id's branch.
@@ -440,12 +444,11 @@ const void *pick_epi(bool part, int adapt) {
                                  : pick_part<BM, BN, WM, WN, NST, OCC, REG, IGEMM_F16>(part);
 }
 // The tile's kernel and its threads. (us, random operands that are not cached:
-// 64 rows of 64 experts, 1024 x 2048: 32 x 256 20.5, 32 x 128 23.5; 4096 rows,
-// 2048 x 1024: 64 x 128 43.5, 64 x 256 47.7, 128 x 128 47.9; 32768 rows, 4096 x 2048:
-// 256 x 256 366, 128 x 256 400, 128 x 128 430; one weight, 8192 x 11008 x 4096: 367,
-// 397, 388, with adapters of rank 16 416, 458, 422, of rank 64 552, 535, 514 (two waves a
-// SIMD have no other work while the adapters' tiles arrive); 2048 x 4096 x 4096, 128
-// tiles of 256 x 256: 57, else 40.)
+// 64 rows of 64 experts, 1024 x 2048: 32 x 256 20.4, 64 x 128 20.9; 4096 rows,
+// 2048 x 1024: 64 x 128 40.7, 128 x 128 46.9; 32768 rows, 4096 x 2048: 256 x 256 360,
+// 128 x 128 410; one weight, 8192 x 11008 x 4096: 365, 370, with adapters of rank 16 394,
+// 406, of rank 64 552, 514 (two waves a SIMD have no other work while the adapters' tiles
+// arrive); 2048 x 4096 x 4096, 128 tiles of 256 x 256: 54, else 39.)
 const void *pick(int bm, int bn, bool reg, bool part, int adapt, int *threads) {
     *threads = bm == 256 ? 512 : 256;
     if (reg)
@@ -506,7 +509,8 @@ int launch_product(const Product &p, const Adapters &ad, int num_cu, void *works
             else
                 shrink_rows<IGEMM_F16><<<g, 256, 0, stream>>>(p, ad, u, c.rpad);
         } else {
-            // 32 ranks a workgroup, or 16 where that fills the compute units better.
+            // 32 ranks a workgroup (8192 rows of 4096, rank 64: 49 us, with 16 ranks 55), or
+            // 16 where 32 would leave compute units idle.
             const int64_t blocks = ceil_div(p.rows, kShrinkRows);
             const bool two = ad.rank > 16 && blocks * ceil_div(ad.rank, 32) >= num_cu;
             const dim3 g((unsigned)blocks, (unsigned)ceil_div(ad.rank, two ? 32 : 16), kShrinkTurns);

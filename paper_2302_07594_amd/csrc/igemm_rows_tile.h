@@ -14,6 +14,9 @@
 //   * the sums are int32 and exact (k <= 131071); they are scaled in float,
 //     turned to rows of 16-byte pieces through LDS and stored once, where the
 //     raw sums would cost two more passes over four bytes an element.
+// Few rows an expert are bound by reading B (512 tokens of 8 slots, 64 experts of 2048 x
+// 1024, bf16: 42 us, 3.5 TB/s), many by the matrix instructions and the power they draw
+// (32768 rows, 64 experts of 4096 x 2048: 360 us, 1520 TOPS).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -725,7 +728,7 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
         // The adapters from memory: fragments of u and `up` straight into registers, the
         // next 16 ranks' on their way while these are multiplied (all blocks' first
         // ones from the start; staged as k-tiles, which is the 256-row tiles' way, 2048 x
-        // 4096 x 4096 with rank 64 took 56 us against 52).
+        // 4096 x 4096 with rank 64, 54 us, took 4 us more).
         struct Piece {
             float u[8];
             u32 w[TN][4];
