@@ -283,6 +283,20 @@ def test_grouped_far_weights():
     assert np.array_equal(got.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("rows", [700, 6])
+def test_grouped_far_output(rows):
+    """Rows of out past 4 GiB, gathered from one row and scattered in turned order."""
+    n, ld = 48, 1 << 22 if rows > 6 else (1 << 22) - 3
+    flat = torch.zeros((rows - 1) * ld + n, dtype=BF16, device="cuda")
+    out = flat.as_strided((rows, n), (ld, 1))
+    order = torch.arange(rows - 1, -1, -1, dtype=torch.int32, device="cuda")
+    a = torch.arange(rows, device="cuda").remainder(100).to(torch.int8)[:, None].contiguous()
+    b = torch.ones(1, 1, n, dtype=torch.int8, device="cuda")
+    ig.grouped_i8(a, b, torch.tensor([0, rows], dtype=torch.int32).cuda(), order, slots=1,
+                  scatter=True, out=out)
+    assert torch.equal(out, a.to(BF16).expand(rows, n))
+
+
 # ---- the sum of a token's slots -------------------------------------------------
 
 @pytest.mark.parametrize("tokens, top_k, n", [(1, 1, 1), (1, 8, 4096), (7, 3, 33), (130, 2, 1000),
@@ -322,6 +336,20 @@ def test_combine(tokens, top_k, n, dtype, pads):
 
 
 # ---- adapters --------------------------------------------------------------------
+
+def test_combine_far_rows():
+    """Rows of Z, base and out past 4 GiB."""
+    n, ld = 40, (1 << 31) + 8
+    flat = torch.empty(3 * ld + 3 * n, dtype=BF16, device="cuda")
+    Z = flat.as_strided((4, n), (ld, 1))
+    base = flat.as_strided((2, n), (ld, 1), n)
+    out = flat.as_strided((2, n), (ld, 1), 2 * n)
+    Z.copy_(torch.arange(4, device="cuda")[:, None].expand(4, n))
+    base.fill_(8)
+    w = torch.tensor([[1.0, 2.0], [4.0, 8.0]], device="cuda")
+    got = ig.combine(Z, w, base=base, out=out)
+    assert torch.equal(got.float(), torch.tensor([[10.0], [40.0]], device="cuda").expand(2, n))
+
 
 def make_adapters(rng, m, n, k, adapters, rank, wt, every=None):
     A, B = ints(rng, m, k), ints(rng, k, n)
@@ -425,6 +453,36 @@ def test_adapters_wide_range_of_values():
         for scale in (2.0 ** -40, 1.0, 2.0 ** 40):
             sa = np.full(40, scale, np.float32)
             check_adapters(A, B, ids, down, up, sa, None, None, None, F32)
+
+
+@pytest.mark.parametrize("wt", [BF16, F16])
+@pytest.mark.parametrize("k", [9, 500, 512, 513, 1024, 1100, 1536, 2048, 2059, 2560])
+def test_adapters_lengths(k, wt):
+    """Tiles of 512 k in u's product: none to five whole ones, with and without a rest; 16
+    and 33 ranks, more adapters than one workgroup of a block takes."""
+    rng = np.random.default_rng(k)
+    for m, rank, adapters in ((300, 16, 3), (140, 33, 40)):
+        A, B, ids, down, up = make_adapters(rng, m, 40, k, adapters, rank, wt)
+        check_adapters(A, B, ids, down, up, None, None, None, None, F32)
+
+
+@pytest.mark.parametrize("m, n", [(3, 64), (400, 512), (8192, 2048)])
+def test_adapters_far_matrices(m, n):
+    """The second adapter's matrices lie past 4 GiB: few rows, the 128-row tiles, the
+    256-row ones. Sums of ones, exact in every type."""
+    k, rank, far = 64, 16, 5 << 29
+    down = torch.zeros(far + rank * k, dtype=BF16, device="cuda").as_strided(
+        (2, rank, k), (far, k, 1))
+    up = torch.zeros(far + n * rank, dtype=BF16, device="cuda").as_strided(
+        (2, n, rank), (far, rank, 1))
+    down[1] = 1
+    up[0] = up[1] = 1
+    a = torch.ones(m, k, dtype=torch.int8, device="cuda")
+    ids = torch.arange(m, dtype=torch.int32, device="cuda") % 3  # (2: none)
+    got = ig.adapters_i8(a, torch.ones(k, n, dtype=torch.int8, device="cuda"), ids, down, up,
+                         out_dtype=F32)
+    want = torch.where(ids == 1, float(k + k * rank), float(k))[:, None].expand(m, n)
+    assert torch.equal(got, want)
 
 
 @pytest.mark.parametrize("wt", [BF16, F16])
