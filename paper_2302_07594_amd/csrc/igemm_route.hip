@@ -16,8 +16,9 @@
 //
 // Bound by latency: a launch, one round of loads and the search's dependent steps, and
 // straight-line code costs the fetch of its instructions (unrolled or two bits a step the
-// search is slower). 8 tokens of 64 experts with their plan 6 us in one launch; 4096 of
-// 256 in 8 groups 13 us and 9 for the plan; 16384 of 128 18 us and 8.
+// search is slower); for many tokens by the issue of instructions (two workgroups a
+// compute unit are no faster). 8 tokens of 64 experts with their plan 6 us in one launch;
+// 4096 of 256 in 8 groups 13 us and 9 for the plan; 16384 of 128 18.5 us and 8.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
