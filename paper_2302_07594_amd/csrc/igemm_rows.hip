@@ -423,12 +423,6 @@ Choice choose(int64_t rows, int64_t n, int64_t k, int64_t groups, int64_t adapte
     return c;
 }
 
-// Row tiles at most: every group with rows may end inside one.
-int64_t most_tiles(int64_t rows, int64_t groups, int64_t bm) {
-    const int64_t used = groups < rows ? groups : rows;
-    return (rows + used * (bm - 1)) / bm;
-}
-
 template <int BM, int BN, int WM, int WN, int NST, int OCC, bool REG, int ADAPT>
 const void *pick_part(bool part) {
     if (!part) return (const void *)rows_tile<BM, BN, WM, WN, NST, OCC, REG, false, ADAPT>;

@@ -30,6 +30,12 @@ struct Adapters {
     int adapters, rank, type;
 };
 
+// Row tiles of bm rows at most: every group with rows may end inside one.
+inline int64_t most_tiles(int64_t rows, int64_t groups, int64_t bm) {
+    const int64_t used = groups < rows ? groups : rows;
+    return (rows + used * (bm - 1)) / bm;
+}
+
 int launch_route(const igemm_route_desc &d, const void *logits, int64_t ld, const float *bias,
                  int32_t *ids, float *weights, int32_t *offsets, int32_t *order, void *workspace,
                  void *stream);

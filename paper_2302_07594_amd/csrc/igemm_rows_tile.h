@@ -212,34 +212,10 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
     }
 
     // ---- which tile -----------------------------------------------------------
-    const int tiles_n = (p.n + BN - 1) / BN;
-    const int per = (p.groups + 63) / 64;
-    int before;
-    const int row_tiles = wave_tiles(p, BM, per, lane, &before);
-    // Workgroup ids go to the eight XCDs in turn: each takes a contiguous range
-    // of the tiles, so that tiles that run together share A and B in its L2.
-    const int64_t total = (int64_t)row_tiles * tiles_n * slices;
-    int64_t at;
-    {
-        const int64_t q = total >> 3;
-        const int b = (int)blockIdx.x - first;
-        const int r = (int)(total & 7), x = b & 7, i = b >> 3;
-        if (i >= q + (x < r)) return;
-        at = x * q + min(x, r) + i;
-    }
-    const int z = (int)(at % slices), t = (int)(at / slices);
-    const Found f = wave_find(p, BM, per, lane, before, t / tiles_n);
+    const Place at = place_of(p, BM, BN, slices, lane, (int)blockIdx.x - first);
+    const Found f = at.f;
     if (f.cnt == 0) return;
-    // Within a group: eight row tiles at a time, over all columns.
-    int m0, n0;
-    {
-        const int mt = (f.cnt + BM - 1) / BM;
-        const int in = t - f.pre * tiles_n, span = 8 * tiles_n;
-        const int first = in / span * 8, gsize = min(mt - first, 8);
-        const int rest = in - in / span * span;
-        m0 = (first + rest % gsize) * BM;
-        n0 = rest / gsize * BN;
-    }
+    const int m0 = at.m0, n0 = at.n0, z = at.z;
     const int mrows = min(f.cnt - m0, BM);
     const int kbeg = z * kchunk, klen = min(p.k - kbeg, kchunk);
     const int nkt = (klen + BK - 1) / BK;
