@@ -288,6 +288,14 @@ join_slices(Product p, Adapters ad, const float *__restrict__ u, int ks, int rpa
 // before the first is used; a group of `lanes` threads (a power of two) covers a
 // row, or 16 * lanes bytes of it. Slots left out read the token's first slot's
 // row instead, which is at hand, so that no load waits for an id's branch.
+// Whether the v elements from c on lie in a row of n, 0 <= c < n. (c + v may pass an int:
+// the last 16 bytes of a row of 2^31 - 1 elements begin at 2^31 - 8.)
+constexpr __host__ __device__ bool whole_from(int c, int v, int n) { return c <= n - v; }
+static_assert(!whole_from(0x7ffffff8, 8, 0x7fffffff) && whole_from(0x7ffffff0, 8, 0x7fffffff) &&
+                  !whole_from(0x7ffffffc, 4, 0x7fffffff) && !whole_from(0, 8, 7) &&
+                  whole_from(0, 8, 8) && !whole_from(0, 8, 1),
+              "the ends of rows");
+
 template <int T, bool WAVE>
 __global__ void __launch_bounds__(256)
 combine_slots(int64_t tokens, int top_k, int n, const char *Z, int64_t ldz,
@@ -302,7 +310,7 @@ combine_slots(int64_t tokens, int top_k, int n, const char *Z, int64_t ldz,
     if constexpr (WAVE)  // the whole wave has one token: its weights are scalars
         t = (int64_t)__builtin_amdgcn_readfirstlane((int)t);
     if (t >= tokens || c >= n) return;
-    const bool whole = c + V <= n;
+    const bool whole = whole_from(c, V, n);
     auto fetch = [&](const char *row) -> v4i {
         if (whole) return ring::load_u16(row + (int64_t)c * ES);
         return load_elems<ES == 4 ? 1 : 2>(row + (int64_t)c * ES, 0, ES == 4 ? (n - c) * 4 : n - c);
@@ -319,20 +327,20 @@ combine_slots(int64_t tokens, int top_k, int n, const char *Z, int64_t ldz,
         for (int e = 0; e < V; ++e) x[e] = value(b, e);
     }
     const int64_t s0 = t * top_k;
-    for (int j0 = 0; j0 < top_k; j0 += 8) {
+    int64_t s8 = s0;  // the next eight slots; (counted down: j0 + 8 may pass an int)
+    for (int left = top_k; left > 0; left -= 8, s8 += 8) {
         v4i z[8];
         float w[8];
         bool on[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const bool in = j0 + j < top_k;
-            const int64_t s = s0 + (in ? j0 + j : 0);
+            const bool in = j < left;
+            const int64_t s = in ? s8 + j : s0;
             on[j] = in && (ids == nullptr || ids[s] >= 0);
             w[j] = weights[s];
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            z[j] = fetch(Z + (on[j] ? s0 + j0 + j : s0) * ldz * ES);
+        for (int j = 0; j < 8; ++j) z[j] = fetch(Z + (on[j] ? s8 + j : s0) * ldz * ES);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll

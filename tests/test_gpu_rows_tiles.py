@@ -27,3 +27,35 @@ def test_offsets_that_do_not_ascend_over_many_columns():
     torch.cuda.synchronize()
     assert bool((whole[:8] == 7).all()) and bool((whole[-8:] == 7).all())
     assert bool(((out == 1) | (out == 7)).all())
+
+
+# ---- the sum of a token's slots -------------------------------------------------
+
+@pytest.mark.parametrize("n", [2 ** 31 - 1, 2 ** 31 - 8])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_combine_longest_rows(n, dtype):
+    """Rows of the most elements that a call takes: the last 16 bytes of each are whole or
+    not, and what lies behind them is neither read into the sum nor written."""
+    Z = torch.ones(2 * n, dtype=dtype, device="cuda").view(2, n)
+    Z[0, -9:] = torch.arange(2, 11, device="cuda")
+    whole = torch.full((n + 64,), 7.0, dtype=dtype, device="cuda")
+    out = whole[:n].view(1, n)
+    ig.combine(Z, torch.tensor([[1.0, 2.0]], device="cuda"), out=out)
+    assert bool((whole[n:] == 7).all())
+    assert out[0, -9:].tolist() == [float(x + 2) for x in range(2, 11)]
+    assert bool((out[0, :1 << 30] == 3).all()) and bool((out[0, 1 << 30:-9] == 3).all())
+
+
+@pytest.mark.parametrize("top_k", [1, 7, 8, 9, 16, 65])
+@pytest.mark.parametrize("tokens, n", [(1100, 2048), (300, 8192)])
+def test_combine_many_values(tokens, n, top_k):
+    """Workgroups of 256 threads, with slots to the left and right of the eights."""
+    g = torch.Generator(device="cuda").manual_seed(top_k)
+    Z = torch.randn(tokens * top_k, n, generator=g, device="cuda").bfloat16()
+    w = torch.randn(tokens, top_k, generator=g, device="cuda")
+    ids = torch.where(torch.rand(tokens, top_k, generator=g, device="cuda") < 0.2, -1, 3).int()
+    z = Z.double().view(tokens, top_k, n) * torch.where(ids < 0, 0.0, w.double())[:, :, None]
+    want, size = z.sum(1), z.abs().sum(1)
+    got = ig.combine(Z, w, ids=ids)
+    bound = (top_k + 2) * STEP[F32] * size + STEP[BF16] * want.abs() * 1.001 + 2.0 ** -134
+    assert bool(((got.double() - want).abs() <= bound).all())
