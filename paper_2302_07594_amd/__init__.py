@@ -1010,7 +1010,7 @@ def route(logits, top_k, bias=None, groups=1, top_groups=1, group_best=1, score=
     with _on(logits.device, stream) as s:
         new = dict(device=logits.device, dtype=torch.int32)
         ids = torch.empty((tokens, top_k), **new)
-        weights = torch.empty((tokens, top_k), device=logits.device)
+        weights = torch.empty((tokens, top_k), dtype=torch.float32, device=logits.device)
         offsets = torch.empty(experts + 1, **new) if plan else None
         order = torch.empty(tokens * top_k, **new) if plan else None
         ws, ws_bytes = _space("route", workspace, nbytes, logits.device)

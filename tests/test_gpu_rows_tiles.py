@@ -59,3 +59,17 @@ def test_combine_many_values(tokens, n, top_k):
     got = ig.combine(Z, w, ids=ids)
     bound = (top_k + 2) * STEP[F32] * size + STEP[BF16] * want.abs() * 1.001 + 2.0 ** -134
     assert bool(((got.double() - want).abs() <= bound).all())
+
+
+# ---- route -------------------------------------------------------------------
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float16, torch.float64])
+def test_route_under_another_default_type(default):
+    x = torch.randn(40, 70, device="cuda")
+    want = ig.route(x, 5)
+    try:
+        torch.set_default_dtype(default)
+        got = ig.route(x, 5, stream=torch.cuda.current_stream())
+    finally:
+        torch.set_default_dtype(F32)
+    assert all(torch.equal(g, w) and g.dtype == w.dtype for g, w in zip(got, want))

@@ -1,6 +1,7 @@
 """Host-side checks of include/igemm_rows.h (no GPU): the exports, the
 refusals before any HIP call, calls with nothing to do, the workspace queries
 and the reference that the GPU tests compare with."""
+import contextlib
 import ctypes
 import os
 import re
@@ -254,3 +255,27 @@ def test_reference_of_the_gpu_tests_on_hand_cases():
                              [0, 0, 1], None, None, np.array([[9.0], [0.5]]), 0, False, 1,
                              np.zeros((1, 1)))
     assert out.tolist() == [[4.0]] and wrote.tolist() == [True]
+
+
+def test_route_allocates_floats_whatever_the_default_type(monkeypatch):
+    """The weights that the call fills are float32 also where torch's default type is
+    narrower or wider (here without a device: the library's call is replaced)."""
+    seen = []
+
+    @contextlib.contextmanager
+    def on(device, stream):
+        yield 0
+    monkeypatch.setattr(ig, "_on", on)
+    monkeypatch.setattr(ig, "_expect", lambda name, what, t, *a, **kw: t.shape[-1])
+    monkeypatch.setattr(ig, "igemm_route", lambda *a: seen.append(a) or ig.IGEMM_OK)
+    before = torch.get_default_dtype()
+    for default in (torch.bfloat16, torch.float16, torch.float64):
+        try:
+            torch.set_default_dtype(default)
+            ids, weights, offsets, order = ig.route(torch.zeros(4, 8, dtype=torch.float32), 2,
+                                                    stream=0)
+        finally:
+            torch.set_default_dtype(before)
+        assert weights.dtype == torch.float32
+        assert ids.dtype == offsets.dtype == order.dtype == torch.int32
+    assert len(seen) == 3
