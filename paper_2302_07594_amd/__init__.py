@@ -964,8 +964,11 @@ def _space(name, workspace, nbytes, device):
     """(workspace, bytes): the caller's, or one from torch's caching allocator."""
     if workspace is None:
         return (_aligned_workspace(nbytes, device), nbytes) if nbytes > 0 else (None, 0)
-    if not hasattr(workspace, "data_ptr"):
-        raise ValueError(f"{name}: workspace must be None or a tensor")
+    import torch
+    if not isinstance(workspace, torch.Tensor) or workspace.device != device or \
+            not workspace.is_contiguous():
+        raise ValueError(f"{name}: workspace must be None or a contiguous tensor on the "
+                         "operands' device")
     return workspace, workspace.numel() * workspace.element_size()
 
 
@@ -983,7 +986,7 @@ def route(logits, top_k, bias=None, groups=1, top_groups=1, group_best=1, score=
     Returns (ids, weights, offsets, order): int32 and float32 (tokens, top_k), with
     id -1 and weight 0 where no expert is left, and the plan that grouped_i8
     takes, int32 (experts + 1) and (tokens * top_k); plan=False leaves the plan
-    out (None, None). workspace as for gemm_i16 (None or a uint8 tensor)."""
+    out (None, None). workspace: None, or a contiguous tensor on the same device."""
     if stream is None and workspace is None and score in ("softmax", "sigmoid"):
         r = (_native or _load_native()).route(
             logits, top_k, bias, groups, top_groups, group_best, 1 if score == "sigmoid" else 0,

@@ -279,3 +279,16 @@ def test_route_allocates_floats_whatever_the_default_type(monkeypatch):
         assert weights.dtype == torch.float32
         assert ids.dtype == offsets.dtype == order.dtype == torch.int32
     assert len(seen) == 3
+
+
+def test_workspaces_elsewhere_are_refused():
+    """A workspace in host memory, on another device or with gaps is named, not handed to
+    the kernels."""
+    cpu, gpu = torch.device("cpu"), torch.device("cuda", 0)
+    host = torch.zeros(512, dtype=torch.uint8)
+    for ws, device in ((host, gpu), (host.to("meta"), gpu), (host[::2], cpu),
+                       (host[:1].expand(512), cpu), (0x10000, gpu)):
+        with pytest.raises(ValueError, match="route: workspace"):
+            ig._space("route", ws, 256, device)
+    assert ig._space("route", host, 256, cpu) == (host, 512)
+    assert ig._space("route", None, 0, gpu) == (None, 0)
