@@ -166,8 +166,10 @@ int igemm_combine(int64_t tokens, int64_t top_k, int64_t n, int type, const void
  *
  * The first sum is exact; the others are held in 32-bit floating point (u is
  * carried into the second in parts that add up to at least 22 bits of its row's
- * largest value), and the result is rounded to `type` once. Nothing of an
- * adapter, infinities and NaN included, reaches the rows of another.
+ * largest value, or to 2^-134), and the result is rounded to `type` once. Nothing of
+ * an adapter, infinities and NaN included, reaches the rows of another; in its own
+ * rows they give what the formula gives (but for an infinite `up` against a u below
+ * 2^-100 that is not 0, which may give NaN).
  *
  *   A, scale_a, B, scale_b, out   as for igemm_i8_grouped with one group: m x k,
  *            k x n (ldb), m x n (ldo); scale_a m floats, scale_b n floats, or NULL.

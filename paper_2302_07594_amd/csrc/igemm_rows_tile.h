@@ -42,9 +42,18 @@ constexpr int kStepK = 128;
 __device__ __forceinline__ int as_int(float x) { return __builtin_bit_cast(int, x); }
 __device__ __forceinline__ float as_float(int x) { return __builtin_bit_cast(float, x); }
 
-// 8 values as bf16 parts hi + mid + lo, their leading 8 bits, the next 8 and the last 8:
-// the value exactly (cut, not rounded: the largest floats round to infinity in bf16). An
-// infinite or NaN value is its hi alone.
+// The bits of x with the magnitude one step smaller (0: as it is). Of an infinity it is the
+// largest finite number.
+__device__ __forceinline__ u32 below(float x, bool nonzero) {
+    return __builtin_bit_cast(u32, x) - (nonzero ? 1u : 0u);
+}
+
+// 8 values as bf16 parts hi + mid + lo, cut from the value just below x and from what is
+// then just below the rest: x exactly (8 leading bits, 8 more, the last ones), and no
+// part of a number is 0. An infinite weight therefore makes an infinity of the
+// product's sign of each part, where a part of 0 would make NaN; of an infinite x, the
+// parts are two finite numbers and an infinity. (|x| of 2^-100 or more: lo is at least
+// 2^-32 of it, and bf16 goes down to 2^-133. NaN is NaN in every part.)
 __device__ __forceinline__ void split3(const float *x, v8bf &hi, v8bf &mid, v8bf &lo) {
     u32 h[4], m[4];
 #pragma unroll
@@ -52,17 +61,37 @@ __device__ __forceinline__ void split3(const float *x, v8bf &hi, v8bf &mid, v8bf
         u32 top[2], rest[2];
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            top[q] = __builtin_bit_cast(u32, x[e + q]);
+            const bool nonzero = x[e + q] != 0.0f;
+            top[q] = below(x[e + q], nonzero);
             const float r = x[e + q] - __builtin_bit_cast(float, top[q] & 0xffff0000u);
-            rest[q] = r == r ? __builtin_bit_cast(u32, r) : 0u;
-            lo[e + q] = (__bf16)(__builtin_bit_cast(float, rest[q]) -
-                                 __builtin_bit_cast(float, rest[q] & 0xffff0000u));
+            rest[q] = below(r, nonzero);
+            lo[e + q] = (__bf16)(r - __builtin_bit_cast(float, rest[q] & 0xffff0000u));
         }
         h[e / 2] = perm(top[1], top[0], 0x07060302u);
         m[e / 2] = perm(rest[1], rest[0], 0x07060302u);
     }
     hi = __builtin_bit_cast(v8bf, h);
     mid = __builtin_bit_cast(v8bf, m);
+}
+
+// 8 float16 values as bf16 parts hi + lo, exactly: their leading 8 bits and the last 3. An
+// infinite or NaN value is its hi alone. (lo may be 0: it is multiplied only with the
+// upper two parts of split3, which are finite.)
+__device__ __forceinline__ void split2(v8hf x, v8bf &hi, v8bf &lo) {
+    u32 h[4];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        u32 top[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const float f = (float)x[e + q];
+            top[q] = __builtin_bit_cast(u32, f);
+            const float r = f - __builtin_bit_cast(float, top[q] & 0xffff0000u);
+            lo[e + q] = (__bf16)(r == r ? r : 0.0f);
+        }
+        h[e / 2] = perm(top[1], top[0], 0x07060302u);
+    }
+    hi = __builtin_bit_cast(v8bf, h);
 }
 
 // 8 consecutive 16-bit values of a row of `len`, from element e0 >= 0; zero from
@@ -531,15 +560,8 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
                             b[q] = have >= 2 * q + 2 ? b[q] : (have == 2 * q + 1 ? b[q] & 0xffff : 0);
                     }
                     v1[j] = __builtin_bit_cast(v8bf, b);
-                    if constexpr (ADAPT == IGEMM_F16) {
-                        // a float16 value is two bf16 parts, exactly
-                        const v8hf hf = __builtin_bit_cast(v8hf, b);
-                        float f8[8];
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) f8[q] = (float)hf[q];
-                        v8bf none;
-                        split3(f8, v1[j], v2[j], none);
-                    }
+                    if constexpr (ADAPT == IGEMM_F16)
+                        split2(__builtin_bit_cast(v8hf, b), v1[j], v2[j]);
                 }
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
@@ -781,13 +803,7 @@ rows_tile(Product p, Adapters ad, float *__restrict__ u, int ks, int kshrink, in
                     const v4u b4 = {f.w[j][0], f.w[j][1], f.w[j][2], f.w[j][3]};
                     v8bf v1 = __builtin_bit_cast(v8bf, b4), v2;
                     if constexpr (ADAPT == IGEMM_F16) {
-                        // a float16 value is two bf16 parts, exactly
-                        const v8hf hf = __builtin_bit_cast(v8hf, b4);
-                        float h[8];
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) h[q] = (float)hf[q];
-                        v8bf rest;
-                        split3(h, v1, v2, rest);
+                        split2(__builtin_bit_cast(v8hf, b4), v1, v2);
                         y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v2, u2, y[j], 0, 0, 0);
                         y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v2, u1, y[j], 0, 0, 0);
                     }

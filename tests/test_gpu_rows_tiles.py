@@ -73,3 +73,81 @@ def test_route_under_another_default_type(default):
     finally:
         torch.set_default_dtype(F32)
     assert all(torch.equal(g, w) and g.dtype == w.dtype for g, w in zip(got, want))
+
+
+# ---- adapters ------------------------------------------------------------------
+
+def same_infinities(got, want, bound, what):
+    """Infinities and NaN where the formula has them, and the rest within bound."""
+    g = got.double()
+    for name, f in (("NaN", torch.isnan), ("infinity", torch.isposinf),
+                    ("-infinity", torch.isneginf)):
+        bad = f(g) != f(want)
+        assert not bool(bad.any()), (what, name, int(bad.sum()), bad.nonzero()[:4].tolist(),
+                                     g[bad][:4].tolist(), want[bad][:4].tolist())
+    ok = want.isfinite()
+    assert bool(((g - want).abs() <= bound)[ok].all()), what
+
+
+# u's lower parts, or a float16 weight's second one, are 0 for values of few bits: the sizes
+# run the row kernels and their k slices, tiles of 32, 128 and 256 rows, through
+# registers (odd rows) and by DMA.
+@pytest.mark.parametrize("m, n, k, rank", [
+    (3, 40, 64, 5), (3, 64, 2048, 16), (130, 72, 64, 33), (131, 90, 33, 40), (2048, 2048, 64, 24),
+    (2050, 2047, 65, 24), (4096, 4096, 64, 16)])
+@pytest.mark.parametrize("wt", [BF16, F16])
+def test_adapters_with_infinite_factors(m, n, k, rank, wt):
+    """An infinite weight or an infinite u gives what the formula gives, whichever kernel
+    runs: infinities of the product's sign, NaN for 0 times infinity and for
+    infinities of both signs."""
+    rng = np.random.default_rng(m + n)
+    A = np.zeros((m, k), np.int8)
+    A[:, :4] = rng.choice([-2, -1, 1, 4, 0, 3, 119], (m, 4), p=[.2, .2, .2, .2, .05, .1, .05])
+    B = ints(rng, k, n, lo=-3, hi=3)
+    down = np.zeros((3, rank, k))
+    down[:, np.arange(rank), np.arange(rank) % 4] = rng.choice([0.5, 1.0, -2.0, 1.7], (3, rank))
+    up = rng.choice([0.0, 1.0, -0.5, 0.7], (3, n, rank))
+    up[0, :, 0] = rng.choice([1.0, np.inf, -np.inf, 0.3], n)
+    up[1, : n // 2, rank - 1] = np.inf
+    down, up = torch.from_numpy(down).to(wt), torch.from_numpy(up).to(wt)
+    scaling = np.array([1.0, 0.75, np.inf], np.float32)
+    ids = (np.arange(m) % 4 - 1).astype(np.int32)
+    got = ig.adapters_i8(cuda(A), cuda(B), cuda(ids), down.cuda(), up.cuda(),
+                         scaling=cuda(scaling), out_dtype=F32)
+    a = torch.from_numpy(A).double()
+    base = (a @ torch.from_numpy(B).double()).cuda()
+    want, reach = base.clone(), torch.zeros_like(base)
+    for w in range(3):
+        rows = torch.from_numpy(np.flatnonzero(ids == w)).cuda()
+        u = (a[rows.cpu()] @ down[w].double().T * float(scaling[w])).cuda()
+        v = up[w].double().cuda()
+        for r in range(rank):     # (a product of infinities by its definition, term by term)
+            term = u[:, r:r + 1] * v[None, :, r]
+            want[rows] += term
+            reach[rows] += term.abs()
+    bound = want.abs() * 8 * STEP[F32] + 4 * STEP[F32] * base.abs() + \
+        (k + rank + 8) * STEP[F32] * reach + 2.0 ** -22 * reach
+    same_infinities(got, want, bound, (m, n, k, rank, wt))
+
+
+@pytest.mark.parametrize("m", [3, 130, 4096])
+@pytest.mark.parametrize("wt", [BF16, F16])
+def test_adapters_with_small_u(m, wt):
+    """u down to the smallest floats, of one bit and of 24: within 2^-134, and infinite
+    against an infinite weight down to 2^-100."""
+    n = 4096 if m == 4096 else 64
+    a = torch.ones(m, 4, dtype=torch.int8, device="cuda")
+    b = torch.zeros(4, n, dtype=torch.int8, device="cuda")
+    ids = torch.zeros(m, dtype=torch.int32, device="cuda")
+    down = torch.zeros(1, 16, 4, dtype=wt, device="cuda")
+    down[:, 0, 0] = 1
+    up = torch.zeros(1, n, 16, dtype=wt, device="cuda")
+    up[:, : n // 2, 0], up[:, n // 2:, 0] = 1, INF
+    for e in (0, -50, -100, -101, -110, -126, -133, -149):
+        for mantissa in (1.0, 1.0 + 2.0 ** -23, 2.0 - 2.0 ** -23, 1.5):
+            u = np.float32(mantissa * 2.0 ** e)
+            got = ig.adapters_i8(a, b, ids, down, up, out_dtype=F32,
+                                 scaling=torch.tensor([u], dtype=F32, device="cuda"))
+            left, right = got[:, : n // 2], got[:, n // 2:]
+            assert bool(((left.double() - float(u)).abs() <= 2.0 ** -134).all()), (e, mantissa)
+            assert e < -100 or bool((right == INF).all()), (e, mantissa)
