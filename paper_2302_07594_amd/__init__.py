@@ -941,6 +941,9 @@ def _expect(name, what, t, dtypes, shape, device, rows=True):
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} has no backward pass: call it under torch.no_grad() or detach "
                          f"{what}")
+    if t.is_floating_point() and \
+            torch.autograd.forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{name} has no forward-mode derivative: detach {what}")
     if t.numel() == 0:
         return max(t.shape[-1], 1)
     if not rows:

@@ -266,12 +266,16 @@ PyObject *conv2d(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
 
 // ---- products whose rows choose their weights --------------------------------------
 
+// Whether a gradient, or a derivative along a tangent, would be asked of what is made of t.
+bool wants_derivative(const at::Tensor &t) {
+    return (t.requires_grad() && c10::GradMode::is_enabled()) || t._fw_grad(/*level=*/0).defined();
+}
 // None, or a plain tensor: *t stays null for None.
 bool plain_or_none(PyObject *o, at::ScalarType dt, int64_t dim, const at::Tensor **t) {
     *t = nullptr;
     if (o == Py_None) return true;
     *t = plain(o, dt, dim);
-    return *t != nullptr && !((*t)->requires_grad() && c10::GradMode::is_enabled());
+    return *t != nullptr && !wants_derivative(**t);
 }
 // A plain float, bfloat16 or half tensor that no gradient is asked of; its igemm_type
 // in *type.
@@ -283,7 +287,7 @@ const at::Tensor *plain_real(PyObject *o, int64_t dim, int *type) {
     else if (dt == at::kHalf) *type = IGEMM_F16;
     else return nullptr;
     const at::Tensor *t = plain(o, dt, dim);
-    return t && !(t->requires_grad() && c10::GradMode::is_enabled()) ? t : nullptr;
+    return t && !wants_derivative(*t) ? t : nullptr;
 }
 // A dense tensor of one or two dimensions of these extents (null: fine).
 bool dense(const at::Tensor *t, int64_t d0, int64_t d1 = -1) {

@@ -7,7 +7,8 @@ import torch
 
 import paper_2302_07594_amd as ig
 import rows_reference as ref
-from test_gpu_rows import BF16, F16, F32, INF, STEP, check_grouped, close, cuda, ints, rounded, split
+from test_gpu_rows import (BF16, F16, F32, INF, STEP, check_grouped, close, cuda, ints, rounded,
+                           split)
 
 pytestmark = pytest.mark.gpu
 
@@ -151,3 +152,49 @@ def test_adapters_with_small_u(m, wt):
             left, right = got[:, : n // 2], got[:, n // 2:]
             assert bool(((left.double() - float(u)).abs() <= 2.0 ** -134).all()), (e, mantissa)
             assert e < -100 or bool((right == INF).all()), (e, mantissa)
+
+
+# ---- autograd ------------------------------------------------------------------
+
+def layer_calls():
+    """(name of an operand, the call with it, the operand) of each call, plain and with a
+    stream (the binding's way and the Python code's)."""
+    d = dict(device="cuda")
+    a = torch.ones(6, 32, dtype=torch.int8, **d)
+    b = torch.ones(2, 32, 16, dtype=torch.int8, **d)
+    off = torch.tensor([0, 2, 6], dtype=torch.int32, **d)
+    ids = torch.zeros(6, dtype=torch.int32, **d)
+    sa, w = torch.rand(6, **d), torch.rand(3, 2, **d)
+    z, y = torch.rand(6, 16, **d), torch.rand(3, 16, **d)
+    down, up = torch.rand(1, 8, 32, **d).bfloat16(), torch.rand(1, 16, 8, **d).bfloat16()
+    scaling = torch.rand(1, **d)
+    out = torch.zeros(6, 16, **d)
+    for kw in ({}, {"stream": torch.cuda.current_stream()}):
+        yield "logits", lambda t, kw=kw: ig.route(t, 2, **kw)[1], torch.rand(5, 9, **d)
+        yield "bias", lambda t, kw=kw: ig.route(torch.rand(5, 9, **d), 2, bias=t, **kw)[0], \
+            torch.rand(9, **d)
+        yield "scale_a", lambda t, kw=kw: ig.grouped_i8(a, b, off, scale_a=t, out=out, **kw), sa
+        yield "out", lambda t, kw=kw: ig.grouped_i8(a, b, off, out=t, **kw), z
+        yield "Z", lambda t, kw=kw: ig.combine(t, w, out=y, **kw), z
+        yield "weights", lambda t, kw=kw: ig.combine(z, t, out=y, **kw), w
+        yield "base", lambda t, kw=kw: ig.combine(z, w, base=t, out=t.detach().clone(), **kw), y
+        yield "out", lambda t, kw=kw: ig.combine(z, w, out=t, **kw), y.clone()
+        for name, t in (("down", down), ("up", up), ("scaling", scaling)):
+            yield name, lambda t, kw=kw, name=name: ig.adapters_i8(
+                a, b[0], out=out, **dict(dict(ids=ids, down=down, up=up, scaling=scaling),
+                                         **{name: t}), **kw), t
+        yield "out", lambda t, kw=kw: ig.adapters_i8(a, b[0], ids, down, up, out=t, **kw), z.clone()
+
+
+def test_no_tangent_is_dropped_in_silence():
+    fw = torch.autograd.forward_ad
+    for name, call, t in layer_calls():
+        with fw.dual_level():
+            dual = fw.make_dual(t, torch.ones_like(t))
+            with pytest.raises(ValueError, match=f"detach {name}"):
+                call(dual)
+            with torch.no_grad(), pytest.raises(ValueError, match=f"detach {name}"):
+                call(dual)
+            call(dual.detach())
+            call(t)
+        call(t)
