@@ -956,6 +956,13 @@ def _expect(name, what, t, dtypes, shape, device, rows=True):
     return ld
 
 
+def _wrote(t):
+    """Autograd's note that t has been written (what it saved of t is out of date)."""
+    import torch
+    if not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+
+
 def _c_int(name, x) -> int:
     """An argument that the C call takes as an int (ctypes would wrap a larger one)."""
     if not -2 ** 31 <= int(x) < 2 ** 31:
@@ -1084,6 +1091,7 @@ def grouped_i8(A, B, offsets, order=None, scale_a=None, scale_b=None, slots=0, s
                               out, ldo, ws, ws_bytes, s)
     if st != IGEMM_OK:
         raise IgemmError(st, "grouped_i8")
+    _wrote(out)
     return out
 
 
@@ -1121,6 +1129,7 @@ def combine(Z, weights, ids=None, base=None, out=None, stream=None):
                            ids, base, ld_base, out, ldo, s)
     if st != IGEMM_OK:
         raise IgemmError(st, "combine")
+    _wrote(out)
     return out
 
 
@@ -1189,4 +1198,5 @@ def adapters_i8(A, B, ids=None, down=None, up=None, scale_a=None, scale_b=None, 
                                ws_bytes, s)
     if st != IGEMM_OK:
         raise IgemmError(st, name)
+    _wrote(out)
     return out

@@ -270,6 +270,10 @@ PyObject *conv2d(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
 bool wants_derivative(const at::Tensor &t) {
     return (t.requires_grad() && c10::GradMode::is_enabled()) || t._fw_grad(/*level=*/0).defined();
 }
+// Autograd's note that t has been written.
+void wrote(const at::Tensor &t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 // None, or a plain tensor: *t stays null for None.
 bool plain_or_none(PyObject *o, at::ScalarType dt, int64_t dim, const at::Tensor **t) {
     *t = nullptr;
@@ -420,6 +424,7 @@ PyObject *grouped(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
                                   lda, data<float>(sa), data<int8_t>(b), ldb, stride_b,
                                   data<float>(sb), out->data_ptr(), ldo, wp, wb, stream);
     }
+    if (st == IGEMM_OK) wrote(*out);
     return status(st);
     END_HANDLE_TH_ERRORS
 }
@@ -449,6 +454,7 @@ PyObject *combine(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
                            data<int32_t>(ids), data<void>(base), ld_base, out->data_ptr(), ldo,
                            stream);
     }
+    if (st == IGEMM_OK) wrote(*out);
     return status(st);
     END_HANDLE_TH_ERRORS
 }
@@ -502,6 +508,7 @@ PyObject *adapters(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
                                    stride_d, up->data_ptr(), ldu, stride_u, data<int32_t>(ranks),
                                    data<float>(scaling), out->data_ptr(), ldo, wp, wb, stream);
     }
+    if (st == IGEMM_OK) wrote(*out);
     return status(st);
     END_HANDLE_TH_ERRORS
 }

@@ -198,3 +198,20 @@ def test_no_tangent_is_dropped_in_silence():
             call(dual.detach())
             call(t)
         call(t)
+
+
+def test_outputs_that_autograd_saved():
+    """A backward pass over a value that a call has overwritten is refused by torch."""
+    for name, call, t in layer_calls():
+        if name != "out":
+            continue
+        version = t._version
+        x = torch.rand_like(t).requires_grad_()
+        y = (x * t).sum()                  # t is saved for x's gradient
+        with torch.no_grad():
+            call(t)
+        assert t._version == version + 1
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+        with torch.inference_mode():
+            call(torch.empty_like(t))
