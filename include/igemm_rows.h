@@ -3,8 +3,8 @@
  * MI355X (gfx950): the routing of tokens to experts, the experts' int8 products,
  * the sum of a token's results, and a shared int8 projection beside which each
  * row has the low-rank adapter of its request (inference of language models
- * with int8 weights). Part of the library of igemm.h, whose status codes,
- * igemm_strerror and igemm_version apply.
+ * with int8 weights). Part of the library of igemm.h (from igemm_version 500 on),
+ * whose status codes and igemm_strerror apply.
  *
  * Operands and results are DEVICE pointers owned by the caller. Checks,
  * asynchrony and errors are those of igemm.h: arguments are checked on the host

@@ -292,3 +292,10 @@ def test_workspaces_elsewhere_are_refused():
             ig._space("route", ws, 256, device)
     assert ig._space("route", host, 256, cpu) == (host, 512)
     assert ig._space("route", None, 0, gpu) == (None, 0)
+
+
+def test_version_counts_these_calls():
+    """A program can tell from the version that the library has them."""
+    text = open(os.path.join(ROOT, "include", "igemm_rows.h")).read()
+    assert "igemm_version 500" in text
+    assert ig.igemm_version() >= 500
