@@ -176,8 +176,12 @@ __device__ int route_token(const igemm_route_desc &d, int64_t t, const float (&l
     }
     auto score = [&](float x) -> double {  // before the division by total
         if (d.score == IGEMM_SOFTMAX) return exp((double)x - (double)top);
-        // (beyond -709 exp overflows and the score is 0)
-        return x > -709.0f ? reciprocal(1.0 + exp(-(double)x)) : 0.0;
+        // (Below -40 the 1 beside exp(-x) is less than half a step of 64 bits, and exp(-x)
+        // comes to the end of reciprocal's range. From -709.7827 on it is infinite, the
+        // score 0.)
+        const bool low = x < -40.0f;
+        const double y = exp(low ? (double)x : -(double)x);
+        return low ? (x > -709.7827f ? y : 0.0) : reciprocal(1.0 + y);
     };
     if constexpr (WIDE) {
         // One copy of exp for all registers, through the scratch (rolled: what a wave

@@ -7,8 +7,8 @@ import torch
 
 import paper_2302_07594_amd as ig
 import rows_reference as ref
-from test_gpu_rows import (BF16, F16, F32, INF, STEP, check_grouped, close, cuda, ints, rounded,
-                           split)
+from test_gpu_rows import (BF16, F16, F32, INF, STEP, check_adapters, check_grouped, check_route,
+                           close, cuda, ints, make_adapters, rounded, split)
 
 pytestmark = pytest.mark.gpu
 
@@ -74,6 +74,21 @@ def test_route_under_another_default_type(default):
     finally:
         torch.set_default_dtype(F32)
     assert all(torch.equal(g, w) and g.dtype == w.dtype for g, w in zip(got, want))
+
+
+@pytest.mark.parametrize("bias", [False, True])
+def test_route_smallest_sigmoids(bias):
+    """Logits whose sigmoid lies at the end of 64-bit floating point: in the order of their
+    scores, with the weights of a normalised choice."""
+    g = torch.Generator().manual_seed(5)
+    x = -(709.7 - 0.6 * torch.rand(40, 64, generator=g))
+    x[20:] = -(300.0 + 400.0 * torch.rand(20, 64, generator=g))
+    x[38] = -(705.0 + 10.0 * torch.rand(64, generator=g))
+    x[39] = -41.0 + 2.0 * torch.rand(64, generator=g)
+    b = torch.zeros(64) if bias else None
+    check_route(x.cuda(), 6, bias=b, groups=4, top_groups=2, group_best=2, score="sigmoid")
+    if bias:
+        check_route(x.cuda(), 6, bias=b, score="sigmoid")
 
 
 # ---- adapters ------------------------------------------------------------------
