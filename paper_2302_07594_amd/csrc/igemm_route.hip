@@ -97,9 +97,9 @@ __device__ __forceinline__ double wave_sum(double x) {
     return read_lane(x, 63);
 }
 
-// 1 / x for x from 1e-290 to 1e290: the hardware's estimate and two Newton steps, within two
-// units of the last place (the compiler's division, three times the instructions, also
-// covers what x cannot be here).
+// 1 / x for x from 1e-290 to 1.79e308: the hardware's estimate and two Newton steps, within
+// two units of the last place, those of numbers below the normal range from 4.5e307 on (the
+// compiler's division, three times the instructions, also covers what x cannot be here).
 __device__ __forceinline__ double reciprocal(double x) {
     double r = __builtin_amdgcn_rcp(x);
     r = fma(fma(-x, r, 1.0), r, r);
@@ -176,12 +176,8 @@ __device__ int route_token(const igemm_route_desc &d, int64_t t, const float (&l
     }
     auto score = [&](float x) -> double {  // before the division by total
         if (d.score == IGEMM_SOFTMAX) return exp((double)x - (double)top);
-        // (Below -40 the 1 beside exp(-x) is less than half a step of 64 bits, and exp(-x)
-        // comes to the end of reciprocal's range. From -709.7827 on it is infinite, the
-        // score 0.)
-        const bool low = x < -40.0f;
-        const double y = exp(low ? (double)x : -(double)x);
-        return low ? (x > -709.7827f ? y : 0.0) : reciprocal(1.0 + y);
+        // (from -709.7827 on exp overflows and the score is 0)
+        return x > -709.7827f ? reciprocal(1.0 + exp(-(double)x)) : 0.0;
     };
     if constexpr (WIDE) {
         // One copy of exp for all registers, through the scratch (rolled: what a wave
