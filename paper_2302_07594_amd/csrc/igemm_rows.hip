@@ -35,7 +35,7 @@ shrink_rows(Product p, Adapters ad, float *__restrict__ u, int rpad) {
 // a compute unit (at least 8 us of reading A there). The block's adapters are shared
 // out to gridDim.z workgroups, each of which takes its own one after the other:
 // where one request ends and the next begins, a block has two.
-constexpr int kShrinkRows = 32, kShrinkTile = 512, kShrinkTurns = 3;
+constexpr int kShrinkTile = 512, kShrinkTurns = 3;
 template <int T, int NR>
 __global__ void __launch_bounds__(512, NR == 1 ? 4 : 2)
 shrink_tiles(Product p, Adapters ad, float *__restrict__ u, int rpad) {
@@ -367,69 +367,8 @@ combine_slots(int64_t tokens, int top_k, int n, const char *Z, int64_t ldz,
 
 // ---- choices --------------------------------------------------------------------------
 
-constexpr int kShrinkK = 1024;  // k a workgroup of a sliced product's shrink_row
-
-struct Choice {
-    int bm, bn;       // tile
-    int slices, kchunk;
-    bool by_row;      // u: a workgroup a row (and k slice, where the product is
-    int ks, rpad;     // sliced: ks of kShrinkK), else blocks of 32 rows
-    int64_t u_bytes, part_bytes;
-};
-
-int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // A grid has fewer than 2^32 threads.
 bool launchable(int64_t blocks, int threads) { return blocks <= 0xffffffffll / threads; }
-
-// By sizes alone, so that the workspace can be sized before the operands exist.
-// What the device will find is taken to be even: `used` groups of `avg` rows.
-Choice choose(int64_t rows, int64_t n, int64_t k, int64_t groups, int64_t adapters, int64_t rank,
-              int num_cu) {
-    Choice c = {};
-    const int64_t used = groups < rows ? groups : rows;
-    const int64_t avg = ceil_div(rows, used);
-    auto tiles = [&](int64_t bm, int64_t bn) { return ceil_div(avg, bm) * used * ceil_div(n, bn); };
-    // share of the last round of workgroups (`at` at a time) that has work
-    auto full = [](int64_t t, int64_t at) { return (double)t / (double)(ceil_div(t, at) * at); };
-    if (avg <= 32) {
-        c.bm = 32, c.bn = 256;
-    } else if (avg <= 64 || tiles(128, 128) < num_cu) {
-        c.bm = 64, c.bn = 128;
-    } else if (avg >= 192 && (adapters == 0 || rank <= 16) &&
-               full(tiles(256, 256), num_cu) >= 0.9 * full(tiles(128, 128), 2 * num_cu)) {
-        c.bm = 256, c.bn = 256;
-    } else {
-        c.bm = 128, c.bn = 128;
-    }
-    // Fewer tiles than compute units: narrower and shorter ones, then k slices, with
-    // adapters for few rows only (join_slices reads `up` once a row).
-    c.by_row = adapters > 0 && rank > 0 && rows * rank <= 4096;
-    const bool adapt = adapters > 0 && rank > 0;
-    int64_t slices = 1;
-    if (c.bm <= 64 && tiles(c.bm, c.bn) < num_cu) {
-        c.bn = 128;
-        if (adapt && !c.by_row) c.bm = 32;
-    }
-    if (c.bm <= 64 && tiles(c.bm, c.bn) < num_cu && (!adapt || c.by_row)) {
-        const int64_t t = tiles(c.bm, 128);
-        if (2 * t <= num_cu) slices = num_cu / t;
-        if (slices > k / 256) slices = k / 256;
-        if (slices > 16) slices = 16;
-        if (slices < 1) slices = 1;
-    }
-    int64_t chunk = ceil_div(ceil_div(k, slices), kStepK) * kStepK;
-    if (chunk < kStepK) chunk = kStepK;
-    c.kchunk = (int)chunk;
-    c.slices = k > 0 ? (int)ceil_div(k, chunk) : 1;
-    if (c.slices > 1) c.part_bytes = up256(c.slices * rows * n * 4);
-    if (adapt) {
-        c.rpad = (int)(ceil_div(rank, 32) * 32);  // (a row's 32 ranks: one line)
-        c.ks = c.slices > 1 ? (int)ceil_div(k, kShrinkK) : 1;
-        c.u_bytes = up256(c.ks * rows * c.rpad * 4);
-    }
-    return c;
-}
 
 template <int BM, int BN, int WM, int WN, int NST, int OCC, bool REG, int ADAPT>
 const void *pick_part(bool part) {
@@ -467,12 +406,6 @@ const void *pick(int bm, int bn, bool reg, bool part, int adapt, int *threads) {
 
 }  // namespace
 
-int64_t product_workspace(int64_t rows, int64_t n, int64_t k, int64_t groups, int64_t adapters,
-                          int64_t rank, int num_cu) {
-    const Choice c = choose(rows, n, k, groups, adapters, rank, num_cu);
-    return c.part_bytes + c.u_bytes;
-}
-
 int launch_product(const Product &p, const Adapters &ad, int num_cu, void *workspace,
                    void *stream_) {
     hipStream_t stream = (hipStream_t)stream_;
@@ -480,26 +413,11 @@ int launch_product(const Product &p, const Adapters &ad, int num_cu, void *works
     int32_t *part = (int32_t *)workspace;
     float *u = (float *)((char *)workspace + c.part_bytes);
     const bool sliced = c.slices > 1, adapt = ad.adapters > 0;
-    // By DMA where rows start at 4-byte addresses and the offsets of a whole last
-    // k-tile stay below 4 GiB; else through registers, in tiles that have the
-    // registers for it.
-    const bool reg = (uintptr_t)p.A % 4 != 0 || (uintptr_t)p.B % 4 != 0 || p.lda % 4 != 0 ||
-                     p.ldb % 4 != 0 || p.stride_b % 4 != 0 ||
-                     ((int64_t)p.k + kStepK) * p.ldb > 0xffffffffll ||
-                     (ad.adapters > 0 && c.bm == 256 &&
-                      ((uintptr_t)ad.up % 4 != 0 || ad.ld_up % 2 != 0 || ad.stride_up % 2 != 0 ||
-                       (int64_t)p.rows * c.rpad * 4 > 0x7fffffff));
-    int bm = c.bm, bn = c.bn, threads = 0;
-    if (reg && bm >= 64) bn = 128;
-    if (reg && bm == 256) bm = 128;
-    // (through registers a workgroup waits more for its loads: 13 experts, 1554 rows,
-    // 1111 x 1777, in 32 rows 20.5 us, in 64 24.0)
-    if (reg && bm == 64 && !sliced &&
-        most_tiles(p.rows, p.groups, 64) * ceil_div(p.n, 128) < 2 * num_cu)
-        bm = 32;
-    const void *fn = pick(bm, bn, reg, sliced, adapt ? ad.type : 0, &threads);
+    const Tile t = tile_of(c, p, ad, num_cu);
+    int threads = 0;
+    const void *fn = pick(t.bm, t.bn, t.reg, sliced, adapt ? ad.type : 0, &threads);
     const int64_t first = sliced && adapt ? (int64_t)p.rows * c.ks * (c.rpad / 16) : 0;
-    const int64_t grid = first + most_tiles(p.rows, p.groups, bm) * ceil_div(p.n, bn) * c.slices;
+    const int64_t grid = first + most_tiles(p.rows, p.groups, t.bm) * ceil_div(p.n, t.bn) * c.slices;
     if (fn == nullptr || !launchable(grid, threads) ||
         (adapt && !launchable(ceil_div(p.rows, kShrinkRows), 512)))
         return IGEMM_ENOTSUP;
@@ -511,11 +429,9 @@ int launch_product(const Product &p, const Adapters &ad, int num_cu, void *works
             else
                 shrink_rows<IGEMM_F16><<<g, 256, 0, stream>>>(p, ad, u, c.rpad);
         } else {
-            // 32 ranks a workgroup (8192 rows of 4096, rank 64: 49 us, with 16 ranks 55), or
-            // 16 where 32 would leave compute units idle.
-            const int64_t blocks = ceil_div(p.rows, kShrinkRows);
-            const bool two = ad.rank > 16 && blocks * ceil_div(ad.rank, 32) >= num_cu;
-            const dim3 g((unsigned)blocks, (unsigned)ceil_div(ad.rank, two ? 32 : 16), kShrinkTurns);
+            const bool two = c.shrink_ranks == 32;
+            const dim3 g((unsigned)ceil_div(p.rows, kShrinkRows),
+                         (unsigned)ceil_div(ad.rank, c.shrink_ranks), kShrinkTurns);
             const bool bf = ad.type == IGEMM_BF16;
             const void *sh = two ? bf ? (const void *)shrink_tiles<IGEMM_BF16, 2>
                                       : (const void *)shrink_tiles<IGEMM_F16, 2>

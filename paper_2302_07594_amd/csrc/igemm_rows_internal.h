@@ -30,6 +30,32 @@ struct Adapters {
     int adapters, rank, type;
 };
 
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// The ring of k-tiles: 128 k, one whole line of a row of A.
+constexpr int kStepK = 128;
+constexpr int kShrinkK = 1024;   // k a workgroup of a sliced product's shrink_row
+constexpr int kShrinkRows = 32;  // rows a workgroup of shrink_tiles
+
+// How a product is cut (igemm_rows_plan.cpp).
+struct Choice {
+    int bm, bn;       // tile
+    int slices, kchunk;
+    bool by_row;      // u: a workgroup a row (and k slice, where the product is
+    int ks, rpad;     // sliced: ks of kShrinkK), else blocks of 32 rows and
+    int shrink_ranks; // so many ranks
+    int64_t u_bytes, part_bytes;
+};
+// By sizes alone, so that the workspace can be sized before the operands exist.
+Choice choose(int64_t rows, int64_t n, int64_t k, int64_t groups, int64_t adapters, int64_t rank,
+              int num_cu);
+// The tile that these operands take, and whether through registers.
+struct Tile {
+    int bm, bn;
+    bool reg;
+};
+Tile tile_of(const Choice &c, const Product &p, const Adapters &ad, int num_cu);
+
 // Row tiles of bm rows at most: every group with rows may end inside one.
 inline int64_t most_tiles(int64_t rows, int64_t groups, int64_t bm) {
     const int64_t used = groups < rows ? groups : rows;

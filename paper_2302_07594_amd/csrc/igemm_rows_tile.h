@@ -36,9 +36,6 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef _Float16 v8hf __attribute__((ext_vector_type(8)));
 
-// The ring of k-tiles: 128 k, one whole line of a row of A.
-constexpr int kStepK = 128;
-
 __device__ __forceinline__ int as_int(float x) { return __builtin_bit_cast(int, x); }
 __device__ __forceinline__ float as_float(int x) { return __builtin_bit_cast(float, x); }
 

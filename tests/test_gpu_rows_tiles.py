@@ -1,14 +1,13 @@
-"""The operators of include/igemm_rows.h on the GPU: sizes that run the large tiles
-and the forms that the sizes of test_gpu_rows.py do not reach, against the same
-references (rows_reference.py) with the same tolerances."""
+"""The operators of include/igemm_rows.h on the GPU: sizes that run the large tiles and the
+forms that the sizes of test_gpu_rows.py do not reach, against definitions in float64,
+with that file's tolerances."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2302_07594_amd as ig
-import rows_reference as ref
-from test_gpu_rows import (BF16, F16, F32, INF, STEP, check_adapters, check_grouped, check_route,
-                           close, cuda, ints, make_adapters, rounded, split)
+from rows_tiles import ADAPTERS, GROUPED
+from test_gpu_rows import BF16, F16, F32, INF, STEP, check_route, cuda, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -230,3 +229,133 @@ def test_outputs_that_autograd_saved():
             y.backward()
         with torch.inference_mode():
             call(torch.empty_like(t))
+
+
+# ---- every tile, with values that tell rows, columns and groups apart ---------------
+
+def gpu_ints(g, *shape):
+    return torch.empty(shape, dtype=torch.int8, device="cuda").random_(-128, 128, generator=g)
+
+
+def generator(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def uneven(rng, rows, groups):
+    """Offsets of groups of very different rows, one of them with half of all (more than
+    eight row tiles of the large sizes) and some with none."""
+    share = rng.random(groups) ** 3 * (rng.random(groups) < 0.8)
+    share[rng.integers(groups)] = share.sum() + 0.1
+    cuts = np.floor(np.cumsum(share / share.sum())[:-1] * rows).astype(np.int64)
+    return np.concatenate([[0], cuts, [rows]]).astype(np.int32)
+
+
+def exact_grouped(a, b, offsets, order, sa, sb, slots, scatter, out):
+    """out (float64) where positions lead, by exact products in float64."""
+    for g in range(b.shape[0]):
+        i = torch.arange(int(offsets[g]), int(offsets[g + 1]), device="cuda")
+        if len(i) == 0:
+            continue
+        s = i if order is None else order[i].long()
+        ra = i if slots == 0 else s // slots
+        y = a[ra].double() @ b[g].double()
+        y = y * sa.double()[ra, None] * sb.double()[g]
+        out[s if scatter else i] = y
+    return out
+
+
+def within(got, want, bound, what=""):
+    bad = ~((got.double() - want).abs() <= bound)
+    assert not bool(bad.any()), (what, int(bad.sum()), bad.nonzero()[:4].tolist(),
+                                 got[bad][:4].tolist(), want[bad][:4].tolist())
+
+
+@pytest.mark.parametrize("way", ["plain", "gather", "scatter"])
+@pytest.mark.parametrize("rows, n, k, groups", GROUPED)
+def test_grouped_tiles(rows, n, k, groups, way):
+    rng, g = np.random.default_rng(rows + n + k), generator(rows * 7 + n)
+    dtype = {"plain": F32, "gather": BF16, "scatter": F16}[way]
+    offsets = uneven(rng, rows, groups)
+    slots = 2 if way == "gather" else 0
+    a_rows = (rows + 1) // 2 if slots else rows
+    a, b = gpu_ints(g, a_rows, k), gpu_ints(g, groups, k, n)
+    sa = torch.rand(a_rows, generator=g, device="cuda") * 1e-3 + 1e-4
+    sb = torch.rand(groups, n, generator=g, device="cuda") * 1e-2 + 1e-3
+    order = None if way == "plain" else \
+        torch.randperm(rows, generator=g, device="cuda").int()
+    out = torch.full((rows + 2, n), 7.0, dtype=dtype, device="cuda")
+    got = ig.grouped_i8(a, b, cuda(offsets), order, sa, sb, slots=slots,
+                        scatter=way == "scatter", out=out)
+    assert got is out
+    want = exact_grouped(a, b, offsets, order, sa, sb, slots, way == "scatter",
+                         torch.full(out.shape, 7.0, dtype=torch.float64, device="cuda"))
+    tiny = {F32: 2.0 ** -150, BF16: 2.0 ** -134, F16: 2.0 ** -25}[dtype]
+    within(out, want, want.abs() * (3 * STEP[F32] + STEP[dtype]) * 1.001 + tiny)
+    assert bool((out[rows:] == 7).all())
+
+
+@pytest.mark.parametrize("rows, n, k, groups", [s for s in GROUPED if s[0] >= 900])
+def test_projection_tiles(rows, n, k, groups):
+    """The projection alone at the same sizes."""
+    g = generator(rows + n)
+    a, b = gpu_ints(g, rows, k), gpu_ints(g, k, n)
+    sa = torch.rand(rows, generator=g, device="cuda") + 0.1
+    sb = torch.rand(n, generator=g, device="cuda") + 0.1
+    want = (a.double() @ b.double()) * sa.double()[:, None] * sb.double()
+    got = ig.adapters_i8(a, b, scale_a=sa, scale_b=sb, out_dtype=F32)
+    within(got, want, want.abs() * 4 * STEP[F32] * 1.001)
+
+
+def adapter_terms(a, b, ids, down, up, sa, sb, ranks, scaling):
+    """As rows_reference.adapters: (out, base, reach, spread), in float64 on the GPU."""
+    a64 = a.double()
+    base = (a64 @ b.double()) * sa.double()[:, None] * sb.double()
+    out, reach, spread = base.clone(), torch.zeros_like(base), torch.zeros_like(base)
+    for w in range(down.shape[0]):
+        i = (ids == w).nonzero().flatten()
+        r = min(max(int(ranks[w]), 0), down.shape[1])
+        if len(i) == 0 or r == 0:
+            continue
+        f = (float(scaling[w]) * sa[i].double())[:, None]
+        d, v = down[w, :r].double(), up[w, :, :r].double()
+        u = a64[i] @ d.T.contiguous() * f
+        out[i] += u @ v.T.contiguous()
+        reach[i] = ((a64[i].abs() @ d.abs().T.contiguous()) * f.abs()) @ v.abs().T.contiguous()
+        spread[i] = u.abs().amax(1, keepdim=True) * v.abs().sum(1)
+    return out, base, reach, spread
+
+
+@pytest.mark.parametrize("wt, dtype", [(BF16, F32), (F16, F32), (BF16, BF16), (F16, F16)])
+@pytest.mark.parametrize("m, n, k, adapters, rank", ADAPTERS)
+def test_adapters_tiles(m, n, k, adapters, rank, wt, dtype):
+    """Random values, scales and ranks; rows in turns, in runs and without an adapter; what
+    lies beyond an adapter's rank, and all of adapter 1, is infinite or NaN."""
+    g = generator(m + n + rank)
+    a, b = gpu_ints(g, m, k), gpu_ints(g, k, n)
+    down = (torch.randn(adapters, rank, k, generator=g, device="cuda") * k ** -0.5).to(wt)
+    up = (torch.randn(adapters, n, rank, generator=g, device="cuda") * 0.3).to(wt)
+    ranks = torch.randint(0, rank + 1, (adapters,), generator=g, device="cuda").int()
+    ranks[0], ranks[-1] = rank, rank + 5
+    ids = torch.randint(-1, adapters + 1, (m,), generator=g, device="cuda").int()
+    ids[m // 3: m // 2] = 0
+    ids[m // 2: m * 3 // 5] = adapters - 1
+    ids[-3:] = torch.tensor([0, -1, 1], device="cuda")
+    beyond = torch.arange(rank, device="cuda") >= ranks[:, None]
+    down.masked_fill_(beyond[:, :, None], float("nan"))
+    up.masked_fill_(beyond[:, None, :], INF)
+    ranks[1] = rank
+    down[1], up[1, ::2], up[1, 1::2] = float("nan"), INF, float("nan")
+    sa = (torch.rand(m, generator=g, device="cuda") + 0.5) * 1e-2
+    sb = (torch.rand(n, generator=g, device="cuda") + 0.5) * 1e-2
+    scaling = torch.rand(adapters, generator=g, device="cuda") + 0.5
+    got = ig.adapters_i8(a, b, ids, down, up, sa, sb, ranks=ranks, scaling=scaling,
+                         out_dtype=dtype)
+    others = torch.where(ids == 1, -1, ids)
+    want, base, reach, spread = adapter_terms(a, b, others, down, up, sa, sb, ranks, scaling)
+    tiny = {F32: 2.0 ** -150, BF16: 2.0 ** -134, F16: 2.0 ** -25}[dtype]
+    bound = (want.abs() * (2 * STEP[F32] + STEP[dtype]) * 1.001 + tiny +
+             4 * STEP[F32] * base.abs() + (k + rank + 8) * STEP[F32] * reach +
+             2.0 ** -22 * spread)
+    keep = ids != 1
+    within(got[keep], want[keep], bound[keep])
+    assert bool(got[~keep].isnan().all())
