@@ -14,7 +14,7 @@
  * out of the arrays described here. As in igemm.h, elements between the rows of an
  * int8, down or up matrix, and bytes of the aligned 16 that hold its first or last
  * element, may be read; their values never matter. Values are the same from run to
- * run, bit for bit.
+ * run, bit for bit (but for rows of out that several positions name).
  */
 #ifndef IGEMM_ROWS_H
 #define IGEMM_ROWS_H
@@ -101,7 +101,8 @@ int igemm_route(const igemm_route_desc *desc, const void *logits, int64_t ld, co
  * The sum is exact, converted to float, multiplied by scale_a, then scale_b
  * (NULL: 1), and rounded to `type` once. out is overwritten. Rows of out that no
  * position reaches, among them those of positions from offsets[groups] on, are
- * left as they were; if two positions name one row of out, one of them is kept.
+ * left as they were. If several positions name one row of out, each of its elements is
+ * one of theirs, not always the same one from run to run.
  * A position whose row of A or out is outside a_rows or out_rows is skipped.
  *
  *   offsets  groups + 1 int32, ascending (or the values of out are not specified);

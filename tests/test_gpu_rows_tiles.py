@@ -7,7 +7,8 @@ import torch
 
 import paper_2302_07594_amd as ig
 from rows_tiles import ADAPTERS, GROUPED
-from test_gpu_rows import BF16, F16, F32, INF, STEP, check_route, cuda, ints
+from test_gpu_rows import (BF16, F16, F32, INF, STEP, check_adapters, check_route, cuda, ints,
+                           make_adapters, strided)
 
 pytestmark = pytest.mark.gpu
 
@@ -359,3 +360,49 @@ def test_adapters_tiles(m, n, k, adapters, rank, wt, dtype):
     keep = ids != 1
     within(got[keep], want[keep], bound[keep])
     assert bool(got[~keep].isnan().all())
+
+
+@pytest.mark.parametrize("rows, n, k", [(6, 300, 1024), (300, 520, 64), (3000, 2052, 32)])
+def test_grouped_rows_that_several_positions_name(rows, n, k):
+    """Each element of such a row is one of the positions' values; all positions on one row,
+    in pairs on the others' last."""
+    g = generator(rows)
+    a, b = gpu_ints(g, rows, k), gpu_ints(g, 2, k, n)
+    offsets = torch.tensor([0, rows // 3, rows], device="cuda").int()
+    order = torch.zeros(rows, device="cuda").int()
+    order[rows // 2:] = torch.arange(rows - rows // 2, device="cuda").int() // 2 + 1
+    out = torch.full((rows, n), 0.5, device="cuda")
+    ig.grouped_i8(a, b, offsets, order, scatter=True, out=out)
+    y = torch.cat([a[:rows // 3].double() @ b[0].double(), a[rows // 3:].double() @ b[1].double()])
+    assert bool((y[order == 0] == out[0].double()).any(0).all())
+    for row in range(1, int(order.max()) + 1):
+        assert bool((y[order == row] == out[row].double()).any(0).all())
+    assert bool((out[int(order.max()) + 1:] == 0.5).all())
+
+
+@pytest.mark.parametrize("m, n", [(3, 300), (40, 300), (600, 260)])
+@pytest.mark.parametrize("wt", [BF16, F16])
+def test_adapters_of_the_largest_rank(m, n, wt):
+    rng = np.random.default_rng(m)
+    A, B, ids, down, up = make_adapters(rng, m, n, 96, 4, 1024, wt)
+    ranks = np.array([1024, 1023, 1009, 1], np.int32)
+    check_adapters(A, B, ids, down, up, None, None, ranks, None, F32)
+
+
+@pytest.mark.parametrize("pad, shift", [(2, 2), (10, 8), (1, 0), (2, 1)])
+@pytest.mark.parametrize("wt", [BF16, F16])
+def test_adapters_strides_of_large_tiles(pad, shift, wt):
+    """`up` with rows and a base at multiples of 4 bytes, which the 256-row tiles take, and
+    at others."""
+    m, n, k, rank = 4000, 4092, 36, 14
+    g = generator(pad)
+    a, b = gpu_ints(g, m, k), gpu_ints(g, k, n)
+    ids = torch.randint(-1, 7, (m,), generator=g, device="cuda").int()
+    down = torch.randn(7, rank, k, generator=g, device="cuda").to(wt)
+    up = strided(torch.randn(7, n, rank, generator=g, device="cuda").to(wt), pad, shift)
+    one, ranks = torch.ones(m, device="cuda"), torch.full((7,), rank)
+    want, base, reach, spread = adapter_terms(a, b, ids, down, up, one, torch.ones(n).cuda(),
+                                              ranks, torch.ones(7))
+    got = ig.adapters_i8(a, b, ids, strided(down, pad, shift), up, out_dtype=F32)
+    within(got, want, want.abs() * 3 * STEP[F32] * 1.001 + 4 * STEP[F32] * base.abs() +
+           (k + rank + 8) * STEP[F32] * reach + 2.0 ** -22 * spread)
