@@ -155,11 +155,18 @@ static int hostile() {
     struct Case {
         int rows, groups, n, bm, bn, slices, kind;
     };
-    const Case cases[] = {{131072, 65536, 8192, 32, 256, 1, 0}, {1 << 22, 65536, 4096, 64, 128, 1, 0},
-                          {1 << 22, 65536, 2432, 64, 128, 1, 0}, {1 << 20, 65536, 4096, 32, 128, 1, 1},
-                          {4096, 60000, 4 << 20, 32, 128, 16, 0}, {100000, 64, 1 << 20, 256, 256, 1, 0},
-                          {100000, 63, 70000, 128, 128, 1, 2},  {2147483136, 65536, 1, 256, 256, 1, 0},
-                          {2147483136, 65536, 1, 128, 128, 1, 2}, {50000, 1000, 100000, 64, 128, 16, 1}};
+    const Case cases[] = {
+        {131072, 65536, 8192, 32, 256, 1, 0},
+        {1 << 22, 65536, 4096, 64, 128, 1, 0},
+        {1 << 22, 65536, 2432, 64, 128, 1, 0},
+        {1 << 20, 65536, 4096, 32, 128, 1, 1},
+        {4096, 60000, 4 << 20, 32, 128, 16, 0},
+        {100000, 64, 1 << 20, 256, 256, 1, 0},
+        {100000, 63, 70000, 128, 128, 1, 2},
+        {2147483136, 65536, 1, 256, 256, 1, 0},
+        {2147483136, 65536, 1, 128, 128, 1, 2},
+        {50000, 1000, 100000, 64, 128, 16, 1},
+    };
     int some = 0;
     for (const Case &c : cases) {
         prod = {};
