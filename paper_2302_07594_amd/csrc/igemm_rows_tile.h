@@ -15,8 +15,10 @@
 //     turned to rows of 16-byte pieces through LDS and stored once, where the
 //     raw sums would cost two more passes over four bytes an element.
 // Few rows an expert are bound by reading B (512 tokens of 8 slots, 64 experts of 2048 x
-// 1024, bf16: 42 us, 3.5 TB/s), many by the matrix instructions and the power they draw
-// (32768 rows, 64 experts of 4096 x 2048: 360 us, 1520 TOPS).
+// 1024, bf16: 43 us, 3.6 TB/s). Many are bound by how full their row tiles are (32768 rows,
+// 64 experts of 4096 x 2048: 0.81 as routed, 365 us, 1510 TOPS; experts of 512 rows each 320,
+// 1710) and by the short k, whose tiles start and end with nothing else under way (one weight,
+// 8192 x 11008 x 4096: 1940 TOPS).
 #pragma once
 
 #include <hip/hip_runtime.h>
